@@ -1,0 +1,125 @@
+/*
+ * Model operators of a pipeline stage (libssn.so): what a Llama-style stage of the paper's model
+ * (grouped-query attention, rotary positions, query/key norm: the model table of the appendix)
+ * computes between its library matrix products, next to the boundary codec of ssn.h.
+ *
+ *   stage_qk_rope_*       the norm of every query and key head with the rotation by position, forward
+ *                         and backward
+ *   stage_distill_loss    the tail stage's loss against a teacher's top logits, with the logits' gradient
+ *   stage_int8_*          products of a frozen stage in 8-bit integers, scaled per token and channel
+ *
+ * The common rules are those of ssn.h: raw DEVICE pointers owned by the caller, strides counted in
+ * ELEMENTS, nothing allocated, freed or synchronised inside, work enqueued on `stream` (a cudaStream_t
+ * passed as void*) of the current device, host-detectable mistakes refused before a launch, one
+ * element type (ssn_dtype_t) per call unless stated, sums in fp32 or wider and ONE rounding at the end.
+ * Buffers of one call must not overlap unless stated.  A call's result is the same bits every time.
+ */
+#ifndef AGORA_STAGE_H_
+#define AGORA_STAGE_H_
+
+#include "ssn.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- query/key norm with rotary positions ---------------------------------------------------------- */
+
+/* Which columns of a head turn together, i < rot_dim / 2: (i, i + rot_dim / 2), or (2 i, 2 i + 1). */
+typedef enum { STAGE_PAIR_HALVES = 0, STAGE_PAIR_ADJACENT = 1 } stage_pairing_t;
+
+#define STAGE_MAX_HEAD_DIM 256
+
+/*
+ * What every block of a stage shares.  Plain value struct, read on the host during the call.
+ * The table holds one row per position: rot_dim / 2 cosines, then rot_dim / 2 sines.
+ */
+typedef struct stage_qk_rope {
+  int32_t head_dim;     /* D: even, 2 .. STAGE_MAX_HEAD_DIM                                        */
+  int32_t rot_dim;      /* rotated columns [0, rot_dim): even, 0 .. D; the others are only normed  */
+  int32_t dtype;        /* ssn_dtype_t of heads, gradients and gains                               */
+  int32_t pairing;      /* stage_pairing_t                                                         */
+  float eps;            /* >= 0, finite                                                            */
+  int32_t max_pos;      /* rows of the table (ignored when rot_dim is 0)                           */
+  const void *wq;       /* device [D] gain of the query heads, or NULL: ones                       */
+  const void *wk;       /* device [D] gain of the key heads, or NULL: ones                         */
+  const float *table;   /* device [max_pos x rot_dim] fp32, required when rot_dim > 0              */
+  int64_t ldt;          /* >= rot_dim                                                              */
+  int32_t *dev_status;  /* device int32 or NULL                                                    */
+} stage_qk_rope_t;
+
+/*
+ * A rotation table: row p has cos(p theta^(-2 i / rot_dim)) at column i and the sine at column
+ * rot_dim / 2 + i, angles and functions in 64 bits, rounded once.  theta > 0, rot_dim >= 2 and even.
+ */
+ssn_status_t stage_rope_table(float *table, int64_t ldt, int32_t max_pos, int32_t rot_dim, double theta,
+                              void *stream);
+
+/*
+ * For every token t and head h, with x the D values at x[t * token_stride + h * head_stride]:
+ *     n = x / sqrt(mean(x^2) + eps) * w;     y = n with its column pairs (a, b) turned by the angle of pos(t):
+ *     (a cos - b sin, b cos + a sin)
+ *   q, k     [n_tokens x heads x D], D contiguous; any strides >= 0 (views of a fused projection's output,
+ *            head-major buffers, broadcast rows).  0 heads: that tensor is absent and may be NULL.
+ *   q_out, k_out   the same with strides that keep its rows apart.  An output may be its own input
+ *            (same address and strides).
+ *   pos      device int32[n_tokens], or NULL: pos(t) = t mod seq_len (seq_len >= 1 required then).
+ *            A position outside [0, max_pos) takes a ZERO table row (its rotated columns become 0) and ORs
+ *            SSN_DEV_BAD_POS into *dev_status.
+ */
+ssn_status_t stage_qk_rope_forward(const stage_qk_rope_t *op, const void *q, int64_t q_token, int64_t q_head,
+                                   int32_t q_heads, const void *k, int64_t k_token, int64_t k_head, int32_t k_heads,
+                                   void *q_out, int64_t qo_token, int64_t qo_head, void *k_out, int64_t ko_token,
+                                   int64_t ko_head, const int32_t *pos, int64_t n_tokens, int32_t seq_len, void *stream);
+
+/*
+ * The gradients: with g the incoming gradient turned back by the angle, r = 1 / sqrt(mean(x^2) + eps), u = x r,
+ *     dx = r (g w - u mean(g w u)),     dw = sum over tokens and heads of g u
+ *   dq, dk          gradients of the forward outputs (any strides >= 0)
+ *   q, k            the forward INPUTS
+ *   dq_in, dk_in    out, gradients of the inputs; may be dq / dk (same address and strides)
+ *   dwq, dwk        out, fp32 [D] each, overwritten (zeros when there are no rows), or NULL: not wanted
+ *   workspace       of stage_qk_rope_workspace_bytes(), 16-byte aligned; not needed when dwq and dwk are NULL
+ */
+size_t stage_qk_rope_workspace_bytes(const stage_qk_rope_t *op, int64_t n_tokens, int32_t q_heads, int32_t k_heads);
+ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, int64_t dq_token, int64_t dq_head,
+                                    const void *dk, int64_t dk_token, int64_t dk_head, const void *q, int64_t q_token,
+                                    int64_t q_head, int32_t q_heads, const void *k, int64_t k_token, int64_t k_head,
+                                    int32_t k_heads, void *dq_in, int64_t dqi_token, int64_t dqi_head, void *dk_in,
+                                    int64_t dki_token, int64_t dki_head, float *dwq, float *dwk, const int32_t *pos,
+                                    int64_t n_tokens, int32_t seq_len, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/* ---- loss against a teacher's top logits ----------------------------------------------------------- */
+
+#define STAGE_DISTILL_MAX_TOP 1024
+#define STAGE_DISTILL_MIN_TAU 1e-6f
+#define STAGE_DISTILL_MAX_TAU 1e6f
+
+/*
+ * A teacher's K best logits of every token are what crosses a slow link instead of a row of the vocabulary.
+ * With x = logits[t] / tau over the vocabulary and p the softmax of top[t] / tau over the row's entries,
+ *     loss[t]       = weight[t] tau^2 sum_j p_j (log p_j - x[ids[t, j]] + log sum_v exp x_v)
+ *     dlogits[t, v] = weight[t] tau (softmax(x)_v - sum over the j with ids[t, j] = v of p_j)
+ *   logits   [n_tokens x vocab] of dtype, ldl >= vocab
+ *   ids      int32 [n_tokens x top_k], ldi >= top_k, and top, fp32 [n_tokens x top_k], ldt >= top_k: the row's
+ *            entries in any order, 1 <= top_k <= STAGE_DISTILL_MAX_TOP.  An id of -1 is padding; any other id outside
+ *            [0, vocab) ORs SSN_DEV_BAD_ID into *dev_status and counts as padding.  An id may stand there twice.
+ *   weight   fp32 [n_tokens] or NULL: ones
+ *   tau      temperature, STAGE_DISTILL_MIN_TAU .. STAGE_DISTILL_MAX_TAU
+ *   loss     fp32 [n_tokens], out
+ *   dlogits  [n_tokens x vocab] of dtype, ldd >= vocab, out, or NULL: the loss alone.  It may be `logits` itself
+ *            (same address and ldd == ldl).
+ * A row of weight 0, one without entries and one whose entries are all -inf have loss 0 and a gradient of zeros,
+ * whatever their logits hold.  Logits of -inf have probability 0 (a loss of +inf where the teacher gives them any).
+ */
+ssn_status_t stage_distill_loss(const void *logits, int64_t ldl, int32_t dtype, int64_t n_tokens, int64_t vocab,
+                                const int32_t *ids, int64_t ldi, const float *top, int64_t ldt, int32_t top_k,
+                                const float *weight, float tau, float *loss, void *dlogits, int64_t ldd,
+                                int32_t *dev_status, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* AGORA_STAGE_H_ */

@@ -51,6 +51,21 @@ class ssn_codec_t(ctypes.Structure):
     ]
 
 
+STAGE_PAIR_HALVES, STAGE_PAIR_ADJACENT = 0, 1
+PAIRINGS = {"halves": STAGE_PAIR_HALVES, "adjacent": STAGE_PAIR_ADJACENT}
+STAGE_MAX_HEAD_DIM, STAGE_DISTILL_MAX_TOP = 256, 1024
+
+
+class stage_qk_rope_t(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("pairing", ctypes.c_int32), ("eps", ctypes.c_float), ("max_pos", ctypes.c_int32),
+        ("wq", ctypes.c_void_p), ("wk", ctypes.c_void_p),
+        ("table", ctypes.c_void_p), ("ldt", ctypes.c_int64),
+        ("dev_status", ctypes.c_void_p),
+    ]
+
+
 def _load() -> ctypes.CDLL:
     path = buildlib.LIB_PATH
     if not os.path.exists(path):
@@ -65,6 +80,7 @@ LIB_PATH = buildlib.LIB_PATH
 
 _vp, _i64, _i32, _sz = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
 _codec_p = ctypes.POINTER(ssn_codec_t)
+_rope_p = ctypes.POINTER(stage_qk_rope_t)
 _SIGNATURES = {
     "ssn_compress": (_i32, [_codec_p, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp]),
     "ssn_decompress": (_i32, [_codec_p, _vp, _i64, _vp, _vp, _i64, _i32, _vp, _i64, _vp, _vp]),
@@ -103,6 +119,13 @@ _SIGNATURES = {
     "stage_clip_sumsq_list": (_i32, [ctypes.POINTER(_vp), ctypes.POINTER(_i64), ctypes.POINTER(_i32), _i32, _vp, _vp]),
     "stage_clip_scale_list": (_i32, [ctypes.POINTER(_vp), ctypes.POINTER(_i64), ctypes.POINTER(_i32), _i32, _vp,
                                      ctypes.c_float, _vp]),
+    "stage_rope_table": (_i32, [_vp, _i64, _i32, _i32, ctypes.c_double, _vp]),
+    "stage_qk_rope_forward": (_i32, [_rope_p] + [_vp, _i64, _i64, _i32] * 2 + [_vp, _i64, _i64] * 2 + [_vp, _i64, _i32, _vp]),
+    "stage_qk_rope_workspace_bytes": (_sz, [_rope_p, _i64, _i32, _i32]),
+    "stage_qk_rope_backward": (_i32, [_rope_p] + [_vp, _i64, _i64] * 2 + [_vp, _i64, _i64, _i32] * 2 + [_vp, _i64, _i64] * 2
+                               + [_vp, _vp, _vp, _i64, _i32, _vp, _sz, _vp]),
+    "stage_distill_loss": (_i32, [_vp, _i64, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _i32, _vp, ctypes.c_float, _vp, _vp, _i64,
+                                  _vp, _vp]),
     "ssn_status_string": (ctypes.c_char_p, [_i32]),
     "ssn_version": (_i32, []),
     "ssn_launch_count": (_i64, []),
@@ -122,7 +145,7 @@ def declared_symbols(header_dir: Optional[str] = None):
         if fname.endswith(".h"):
             text = open(os.path.join(header_dir, fname)).read()
             text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
-            names += re.findall(r"\b((?:ssn|sparta|stage_clip)_[a-z0-9_]+)\s*\(", text)
+            names += re.findall(r"\b((?:ssn|sparta|stage)_[a-z0-9_]+)\s*\(", text)
     return sorted(set(names))
 
 
@@ -385,3 +408,45 @@ def stage_clip_sumsq_list(tensors, sumsq: int, stream: int = 0) -> None:
 
 def stage_clip_scale_list(tensors, sumsq: int, threshold: float, stream: int = 0) -> None:
     _check(_lib.stage_clip_scale_list(*tensors, sumsq or None, threshold, stream or None), "stage_clip_scale_list")
+
+
+# ---- model operators of a stage (include/agora_stage.h) ----------------------------------------
+# Device addresses as above (0 = NULL).  A heads argument is (address, token stride, head stride).
+def make_qk_rope(head_dim: int, rot_dim: int, dtype: int, pairing: int, eps: float, wq: int = 0, wk: int = 0, table: int = 0,
+                 ldt: int = 0, max_pos: int = 0, dev_status: int = 0) -> stage_qk_rope_t:
+    return stage_qk_rope_t(head_dim=head_dim, rot_dim=rot_dim, dtype=dtype, pairing=pairing, eps=eps, max_pos=max_pos,
+                           wq=wq or None, wk=wk or None, table=table or None, ldt=ldt, dev_status=dev_status or None)
+
+
+def stage_rope_table(table: int, ldt: int, max_pos: int, rot_dim: int, theta: float, stream: int = 0) -> None:
+    """Row p of the fp32 table: cosines, then sines, of p theta^(-2 i / rot_dim)."""
+    _check(_lib.stage_rope_table(table or None, ldt, max_pos, rot_dim, theta, stream or None), "stage_rope_table")
+
+
+def stage_qk_rope_forward(op: stage_qk_rope_t, q, q_heads: int, k, k_heads: int, q_out, k_out, pos: int, n_tokens: int,
+                          seq_len: int, stream: int = 0) -> None:
+    """The norm of every head, then the rotation of its first rot_dim columns by the token's position."""
+    _check(_lib.stage_qk_rope_forward(ctypes.byref(op), *q, q_heads, *k, k_heads, *q_out, *k_out, pos or None, n_tokens,
+                                      seq_len, stream or None), "stage_qk_rope_forward")
+
+
+def stage_qk_rope_workspace_bytes(op: stage_qk_rope_t, n_tokens: int, q_heads: int, k_heads: int) -> int:
+    return int(_lib.stage_qk_rope_workspace_bytes(ctypes.byref(op), n_tokens, q_heads, k_heads))
+
+
+def stage_qk_rope_backward(op: stage_qk_rope_t, dq, dk, q, q_heads: int, k, k_heads: int, dq_in, dk_in, dwq: int, dwk: int,
+                           pos: int, n_tokens: int, seq_len: int, workspace: int = 0, workspace_bytes: int = 0,
+                           stream: int = 0) -> None:
+    """Gradients of the forward call's inputs, and of its gains (fp32) where dwq / dwk are given."""
+    _check(_lib.stage_qk_rope_backward(ctypes.byref(op), *dq, *dk, *q, q_heads, *k, k_heads, *dq_in, *dk_in, dwq or None,
+                                       dwk or None, pos or None, n_tokens, seq_len, workspace or None, workspace_bytes,
+                                       stream or None), "stage_qk_rope_backward")
+
+
+def stage_distill_loss(logits: int, ldl: int, dtype: int, n_tokens: int, vocab: int, ids: int, ldi: int, top: int, ldt: int,
+                       top_k: int, weight: int, tau: float, loss: int, dlogits: int = 0, ldd: int = 0, dev_status: int = 0,
+                       stream: int = 0) -> None:
+    """Loss per token against the teacher's top_k logits; the gradient of the logits too where dlogits is given."""
+    _check(_lib.stage_distill_loss(logits or None, ldl, dtype, n_tokens, vocab, ids or None, ldi, top or None, ldt, top_k,
+                                   weight or None, tau, loss or None, dlogits or None, ldd, dev_status or None, stream or None),
+           "stage_distill_loss")

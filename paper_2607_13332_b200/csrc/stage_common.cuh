@@ -1,0 +1,104 @@
+// What the stage operators (include/agora_stage.h) share: chunked element access, launch geometry, dependent launches.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <atomic>
+
+#include "agora_stage.h"
+#include "codec_mma_launch.h"
+
+namespace ssn {
+
+inline bool aligned_to(const void *p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// SMs of the current device (148 when the runtime does not say)
+inline int stage_sm_count() {
+  static std::atomic<int> cached[64];
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 148;
+  int n = cached[dev].load(std::memory_order_relaxed);
+  if (n == 0) {
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) n = 148;
+    cached[dev].store(n, std::memory_order_relaxed);
+  }
+  return n;
+}
+
+inline ssn_status_t launched(cudaError_t e, int launches = 1) {
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return SSN_ERR_CUDA;
+  }
+  count_launches(launches);
+  return SSN_OK;
+}
+
+// Every stage kernel is launched with launch_dependent: it waits for the kernel in front of it before it touches global
+// memory, and lets the one behind it start its own set-up.
+__device__ __forceinline__ void pdl_enter() {
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");
+}
+
+// V elements of T as one access of V * sizeof(T) = 2 .. 16 bytes
+template <int BYTES> struct RawBytes;
+template <> struct RawBytes<2> { uint16_t v[1]; };
+template <> struct __align__(4) RawBytes<4> { uint32_t v[1]; };
+template <> struct __align__(8) RawBytes<8> { uint32_t v[2]; };
+template <> struct __align__(16) RawBytes<16> { uint32_t v[4]; };
+
+template <typename T, int V> struct Chunk {
+  RawBytes<V * (int)sizeof(T)> raw;
+  __device__ __forceinline__ void load(const T *p) { raw = *reinterpret_cast<const RawBytes<V * (int)sizeof(T)> *>(p); }
+  __device__ __forceinline__ void store(T *p) const { *reinterpret_cast<RawBytes<V * (int)sizeof(T)> *>(p) = raw; }
+  __device__ __forceinline__ float get(int i) const;
+  __device__ __forceinline__ void pack(const float (&x)[V]);
+};
+template <typename T, int V> __device__ __forceinline__ float Chunk<T, V>::get(int i) const {
+  if constexpr (sizeof(T) == 4) {
+    return __uint_as_float(raw.v[i]);
+  } else if constexpr (V == 1) {
+    return __uint_as_float((uint32_t)raw.v[0] << 16);
+  } else {
+    return __uint_as_float((i & 1) ? (raw.v[i >> 1] & 0xffff0000u) : (raw.v[i >> 1] << 16));
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void Chunk<T, V>::pack(const float (&x)[V]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) raw.v[i] = __float_as_uint(x[i]);
+  } else if constexpr (V == 1) {
+    raw.v[0] = __bfloat16_as_ushort(__float2bfloat16_rn(x[0]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; i += 2) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(x[i], x[i + 1]);
+      raw.v[i >> 1] = *reinterpret_cast<const uint32_t *>(&b);
+    }
+  }
+}
+
+// V floats of a 16-byte aligned (V >= 4) or V * 4-byte aligned table row
+template <int V> __device__ __forceinline__ void load_floats(const float *p, float (&x)[V]) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int i = 0; i < V; i += 4) {
+      const float4 f = __ldg(reinterpret_cast<const float4 *>(p + i));
+      x[i] = f.x;
+      x[i + 1] = f.y;
+      x[i + 2] = f.z;
+      x[i + 3] = f.w;
+    }
+  } else if constexpr (V == 2) {
+    const float2 f = __ldg(reinterpret_cast<const float2 *>(p));
+    x[0] = f.x;
+    x[1] = f.y;
+  } else {
+    x[0] = __ldg(p);
+  }
+}
+
+}  // namespace ssn
