@@ -118,6 +118,34 @@ ssn_status_t stage_distill_loss(const void *logits, int64_t ldl, int32_t dtype, 
                                 const float *weight, float tau, float *loss, void *dlogits, int64_t ldd,
                                 int32_t *dev_status, void *stream);
 
+/* ---- products in 8-bit integers -------------------------------------------------------------------- */
+
+#define STAGE_INT8_MAX_INNER 131071   /* 128 * 128 * inner stays below 2^31 */
+
+/*
+ * Rows in 8 bits, one scale each (tokens of an activation, or output channels of a weight, stored [outer x inner]):
+ *     scale[r] = max_i |x[r, i]| / 127 in fp32;    q[r, i] = x[r, i] / scale[r], the EXACT quotient rounded to the nearest
+ * integer, halves to the even one, within [-127, 127].
+ *   x      [rows x cols] of dtype, ldx >= cols;   q  int8 [rows x cols], ldq >= cols;   scale  fp32 [rows]
+ * A row whose scale is 0 (zeros, or values below 127 times the smallest fp32 number) has q = 0.  A row with an infinity
+ * or a NaN has q = 0 and scale NaN, so that its products are NaN.
+ */
+ssn_status_t stage_int8_quantize(const void *x, int64_t ldx, int32_t dtype, int64_t rows, int64_t cols, int8_t *q,
+                                 int64_t ldq, float *scale, void *stream);
+
+/*
+ * A frozen projection:  y[t, o] = (sum_i xq[t, i] wq[o, i]) xs[t] ws[o], the sum in 32-bit integers (exact), then two
+ * products in fp32 and one rounding to dtype.
+ *   xq  int8 [n_tokens x inner], ldx >= inner;  xs  fp32 [n_tokens];  wq  int8 [outer x inner], ldw >= inner;
+ *   ws  fp32 [outer];  y  [n_tokens x outer] of dtype, ldy >= outer;  1 <= inner <= STAGE_INT8_MAX_INNER
+ *   dev_status  device int32 or NULL: SSN_DEV_TIMEOUT when an internal bounded wait ran out (y is invalid then)
+ * Any int8 value may occur, -128 too.  xq and wq rows that start on 16-byte boundaries (address and leading dimension)
+ * are fetched by TMA; others take a slower kernel.
+ */
+ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, const int8_t *wq, int64_t ldw,
+                               const float *ws, int64_t n_tokens, int64_t inner, int64_t outer, void *y, int64_t ldy,
+                               int32_t dtype, int32_t *dev_status, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

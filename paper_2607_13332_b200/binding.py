@@ -53,7 +53,7 @@ class ssn_codec_t(ctypes.Structure):
 
 STAGE_PAIR_HALVES, STAGE_PAIR_ADJACENT = 0, 1
 PAIRINGS = {"halves": STAGE_PAIR_HALVES, "adjacent": STAGE_PAIR_ADJACENT}
-STAGE_MAX_HEAD_DIM, STAGE_DISTILL_MAX_TOP = 256, 1024
+STAGE_MAX_HEAD_DIM, STAGE_DISTILL_MAX_TOP, STAGE_INT8_MAX_INNER = 256, 1024, 131071
 
 
 class stage_qk_rope_t(ctypes.Structure):
@@ -126,6 +126,8 @@ _SIGNATURES = {
                                + [_vp, _vp, _vp, _i64, _i32, _vp, _sz, _vp]),
     "stage_distill_loss": (_i32, [_vp, _i64, _i32, _i64, _i64, _vp, _i64, _vp, _i64, _i32, _vp, ctypes.c_float, _vp, _vp, _i64,
                                   _vp, _vp]),
+    "stage_int8_quantize": (_i32, [_vp, _i64, _i32, _i64, _i64, _vp, _i64, _vp, _vp]),
+    "stage_int8_matmul": (_i32, [_vp, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _i32, _vp, _vp]),
     "ssn_status_string": (ctypes.c_char_p, [_i32]),
     "ssn_version": (_i32, []),
     "ssn_launch_count": (_i64, []),
@@ -450,3 +452,16 @@ def stage_distill_loss(logits: int, ldl: int, dtype: int, n_tokens: int, vocab: 
     _check(_lib.stage_distill_loss(logits or None, ldl, dtype, n_tokens, vocab, ids or None, ldi, top or None, ldt, top_k,
                                    weight or None, tau, loss or None, dlogits or None, ldd, dev_status or None, stream or None),
            "stage_distill_loss")
+
+
+def stage_int8_quantize(x: int, ldx: int, dtype: int, rows: int, cols: int, q: int, ldq: int, scale: int, stream: int = 0) -> None:
+    """Rows in 8 bits: scale = max |x| / 127, q = x / scale rounded to the nearest integer."""
+    _check(_lib.stage_int8_quantize(x or None, ldx, dtype, rows, cols, q or None, ldq, scale or None, stream or None),
+           "stage_int8_quantize")
+
+
+def stage_int8_matmul(xq: int, ldx: int, xs: int, wq: int, ldw: int, ws: int, n_tokens: int, inner: int, outer: int, y: int,
+                      ldy: int, dtype: int, dev_status: int = 0, stream: int = 0) -> None:
+    """y [n_tokens x outer] = (xq wq^T) scaled by xs per token and ws per output channel."""
+    _check(_lib.stage_int8_matmul(xq or None, ldx, xs or None, wq or None, ldw, ws or None, n_tokens, inner, outer, y or None,
+                                  ldy, dtype, dev_status or None, stream or None), "stage_int8_matmul")

@@ -143,8 +143,7 @@ def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight:
         raise ValueError(f"weight: expected {n} contiguous fp32")
     if dlogits is not None and _here(dlogits, logits.dtype, "dlogits").shape != logits.shape:
         raise ValueError("dlogits: expected the shape of the logits")
-    if dev_status is not None:
-        _ints(dev_status, 1, "dev_status")
+    _ints(dev_status, 1, "dev_status")
     loss = torch.empty(n, dtype=torch.float32, device=logits.device)
     st = _lib.stage_distill_loss(logits.data_ptr(), _ld(logits), _CODES[logits.dtype], n, vocab, ids.data_ptr(), _ld(ids),
                                  top.data_ptr(), _ld(top), ids.shape[1], _ptr(weight), temperature, loss.data_ptr(), _ptr(dlogits),
@@ -168,3 +167,43 @@ def distill_loss_grad(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor
         n, vocab = logits.shape
         dlogits = torch.empty((n, max(_ld(logits), vocab)), dtype=logits.dtype, device=logits.device)[:, :vocab]
     return _distill(logits, ids, top, weight, temperature, dlogits, dev_status), dlogits
+
+
+# ---- products in 8-bit integers -----------------------------------------------------------------------------------------------
+def int8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None):
+    """(q, scale): the rows of x (fp32 or bf16) in 8 bits with one fp32 scale each.  q made here has a leading dimension that
+    is a multiple of 16, which is what int8_matmul's TMA kernels need."""
+    if x.dtype not in _CODES:
+        raise ValueError("x: expected fp32 or bf16")
+    rows, cols = _here(x, x.dtype, "x").shape
+    if q is None:
+        q = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=x.device)
+        if q.shape[1] != cols:
+            q = q[:, :cols]
+    elif _here(q, torch.int8, "q").shape != x.shape:
+        raise ValueError("q: expected the shape of x")
+    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    st = _lib.stage_int8_quantize(x.data_ptr(), _ld(x), _CODES[x.dtype], rows, cols, q.data_ptr(), _ld(q), scale.data_ptr(), _stream())
+    binding.check(st, "stage_int8_quantize")
+    return q, scale
+
+
+def int8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, dtype: str = "bf16",
+                out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [n, outer] of dtype = (xq [n, inner] times wq [outer, inner] transposed), scaled by xs [n] and ws [outer]."""
+    n, inner = _here(xq, torch.int8, "xq").shape
+    outer = _here(wq, torch.int8, "wq").shape[0]
+    if wq.shape[1] != inner:
+        raise ValueError(f"wq: expected [outer, {inner}]")
+    for s, rows, what in ((xs, n, "xs"), (ws, outer, "ws")):
+        if _here(s, torch.float32, what).shape != (rows,) or not s.is_contiguous():
+            raise ValueError(f"{what}: expected {rows} contiguous fp32")
+    if out is None:
+        out = torch.empty((n, outer), dtype=_TORCH_DTYPE[dtype], device=xq.device)
+    elif _here(out, _TORCH_DTYPE[dtype], "out").shape != (n, outer):
+        raise ValueError(f"out: expected [{n}, {outer}]")
+    _ints(dev_status, 1, "dev_status")
+    st = _lib.stage_int8_matmul(xq.data_ptr(), _ld(xq), xs.data_ptr(), wq.data_ptr(), _ld(wq), ws.data_ptr(), n, inner, outer,
+                                out.data_ptr(), _ld(out), binding.DTYPES[dtype], _ptr(dev_status), _stream())
+    binding.check(st, "stage_int8_matmul")
+    return out
