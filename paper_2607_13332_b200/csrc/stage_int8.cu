@@ -1,5 +1,6 @@
 // Products in 8-bit integers with scales per token and channel (include/agora_stage.h): quantisation and dispatch.
 #include "stage_common.cuh"
+#include "stage_int8.h"
 
 #include <cmath>
 
@@ -67,16 +68,9 @@ __global__ void __launch_bounds__(kQuantThreads) int8_quantize_kernel(const Quan
 }
 
 // ---- any alignment --------------------------------------------------------------------------------------------------
-struct MatmulArgs {
-  const int8_t *xq, *wq;
-  const float *xs, *ws;
-  void *y;
-  int64_t ldx, ldw, ldy, n, inner, outer;
-};
-
 // 64 tokens x 64 channels per CTA, steps of 32 bytes of the inner dimension as 8 words, dp4a
 template <typename T>
-__global__ void __launch_bounds__(256) int8_general_kernel(const MatmulArgs a) {
+__global__ void __launch_bounds__(256) int8_general_kernel(const Int8Matmul a) {
   __shared__ int xt[64][9], wt[64][9];
   const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
   const int64_t tiles_o = (a.outer + 63) / 64, tiles = (a.n + 63) / 64 * tiles_o;
@@ -118,7 +112,7 @@ __global__ void __launch_bounds__(256) int8_general_kernel(const MatmulArgs a) {
 }
 
 template <typename T>
-cudaError_t launch_general(const MatmulArgs &a, cudaStream_t stream) {
+cudaError_t launch_general(const Int8Matmul &a, cudaStream_t stream) {
   const int64_t tiles = (a.n + 63) / 64 * ((a.outer + 63) / 64), cap = (int64_t)stage_sm_count() * 8;
   return launch_dependent(int8_general_kernel<T>, (unsigned)(tiles < cap ? tiles : cap), 256, 0, stream, 1, a);
 }
@@ -158,8 +152,10 @@ ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, c
   if (ldx > kFar / n_tokens || ldy > kFar / n_tokens || ldw > kFar / outer || n_tokens > kFar / outer) return SSN_ERR_SHAPE;
   if (xq == nullptr || xs == nullptr || wq == nullptr || ws == nullptr || y == nullptr) return SSN_ERR_NULL;
   if (!aligned_to(y, dtype == SSN_F32 ? 4 : 2)) return SSN_ERR_SHAPE;
-  const MatmulArgs a{xq, wq, xs, ws, y, ldx, ldw, ldy, n_tokens, inner, outer};
+  const Int8Matmul a{xq, wq, xs, ws, y, ldx, ldw, ldy, n_tokens, inner, outer, dev_status};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = launch_int8_umma(a, dtype == SSN_F32, stage_sm_count(), s);
+  if (e != cudaErrorNotSupported) return launched(e);
   return launched(dtype == SSN_F32 ? launch_general<float>(a, s) : launch_general<__nv_bfloat16>(a, s));
 }
 
