@@ -2,11 +2,16 @@
 //
 // With m the row's largest logit and L = sum exp((s - m) / tau), everything but the teacher's entries follows from (m, L):
 // the gradient is w tau exp((s - m) / tau) / L, minus w tau p at the teacher's ids.  The loss reads the row once; the
-// gradient reads and writes it once.
+// gradient reads it once more out of L2 and writes it once, so that HBM sees the row read once and written once.
 //
-// Rows are taken 16 bytes at a time from the 16-byte boundary at or before their start (a vocabulary may be odd), the first
-// and last piece element by element.  Sums are fp32 per thread, at most a few dozen terms relative to the thread's own
-// maximum, then over warps and CTAs in a fixed order; the loss itself, a difference of large terms, is put together in 64 bits.
+// What bounds it: HBM for the loss of long rows (2048 x 128256 bf16 in 101 us, 5.2 TB/s).  The gradient (8192 x 128256 bf16 in
+// 0.99 ms, 4.2 TB/s) also waits for its exponentials, two per element on a pipe of 16 lanes per clock and SM (58 % busy), and
+// for the reductions between the passes.  Tried and dropped: the exponentials of a row kept in the registers of a cluster of
+// eight CTAs, so that each is computed once (1.44 ms: 33 of the 37 clusters fit, and 20 warps share too little of a row);
+// a ring of bulk copies with a warp of its own (1.01 ms); registers filled a round ahead (slower, fewer warps).
+//
+// Sums are fp32 per thread, relative to the thread's running maximum, then over warps and CTAs in a fixed order; the loss
+// itself, a difference of large terms, is put together in 64 bits.
 #include "stage_common.cuh"
 
 #include <cmath>
@@ -14,7 +19,7 @@
 namespace ssn {
 namespace {
 
-constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
+constexpr int kMaxWarps = 8, kMaxCluster = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct DistillArgs {
@@ -35,202 +40,367 @@ __device__ __forceinline__ float exp2_approx(float x) {   // 2 ulp; a probabilit
   return y;
 }
 
-// What a set of logits contributes: its maximum and the sum of exp2((s - m) scale) over it
+// What a set of logits contributes: its maximum m and the sum of exp2((s - m) scale) over it, scale = log2(e) / tau.  The
+// difference comes first: s scale - m scale in one fma is an instruction less, but loses everything where the logits are large
+// (a mask of the type's lowest value).
 struct MaxSum {
   float m, l;
 };
-__device__ __forceinline__ MaxSum merge(MaxSum a, MaxSum b, float scale) {
-  const float m = fmaxf(a.m, b.m), at = m == -INFINITY ? 0.f : m;   // two empty sets stay empty
-  return {m, a.l * exp2_approx((a.m - at) * scale) + b.l * exp2_approx((b.m - at) * scale)};
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }   // for an empty set any number will do
+// what turns a sum over a set of maximum m into one from another base; a set without a maximum has no sum (or a NaN)
+__device__ __forceinline__ float rescale(float m, float base, float scale) {
+  return m == -INFINITY ? 0.f : exp2_approx((m - base) * scale);
+}
+// over the lanes of a warp, in an order that does not depend on the lane
+__device__ __forceinline__ MaxSum merge_warp(MaxSum ms, float scale) {
+  float m = ms.m;
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float l = ms.l * rescale(ms.m, base_of(m), scale);
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  return {m, l};
 }
 
-template <typename T> struct Piece {   // 16 bytes of a row
-  static constexpr int E = 16 / (int)sizeof(T);
+// Two fp32 values per instruction
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+__device__ __forceinline__ float2 exponents(float2 s, float base, float scale) {
+  return mul2(add2(s, make_float2(-base, -base)), make_float2(scale, scale));
+}
+
+// 16 bytes of a row
+template <typename T> struct Piece {
+  static constexpr int E = 16 / (int)sizeof(T), kPairs = E / 2;
   Chunk<T, E> c;
-  // elements [first, first + E) of the row; those outside [0, vocab) are -inf
-  __device__ __forceinline__ void load(const T *row, int64_t first, int64_t vocab) {
-    if (first >= 0 && first + E <= vocab) {
-      const uint4 v = *reinterpret_cast<const uint4 *>(row + first);
-      c.raw.v[0] = v.x, c.raw.v[1] = v.y, c.raw.v[2] = v.z, c.raw.v[3] = v.w;
-    } else {
-      float x[E];
+  __device__ __forceinline__ void set(float v) {
+    float x[E];
 #pragma unroll
-      for (int i = 0; i < E; ++i) {
-        x[i] = -INFINITY;
-        if (first + i >= 0 && first + i < vocab) x[i] = to_f32<T>(row[first + i]);
-      }
-      c.pack(x);
-    }
+    for (int i = 0; i < E; ++i) x[i] = v;
+    c.pack(x);
   }
-  __device__ __forceinline__ void store(T *row, int64_t first, int64_t vocab, bool whole) const {
-    if (whole && first >= 0 && first + E <= vocab) {
-      *reinterpret_cast<uint4 *>(row + first) = make_uint4(c.raw.v[0], c.raw.v[1], c.raw.v[2], c.raw.v[3]);
-    } else {
+  __device__ __forceinline__ void load(const void *p, bool last_use) {
+    const uint4 v = last_use ? __ldcs(static_cast<const uint4 *>(p)) : *static_cast<const uint4 *>(p);
+    c.raw.v[0] = v.x, c.raw.v[1] = v.y, c.raw.v[2] = v.z, c.raw.v[3] = v.w;
+  }
+  __device__ __forceinline__ void store(void *p) const { __stcs(static_cast<uint4 *>(p), make_uint4(c.raw.v[0], c.raw.v[1], c.raw.v[2], c.raw.v[3])); }
+  // elements [first, first + E) of a row; those outside [0, vocab) are -inf, and are not written
+  __device__ __forceinline__ void load_some(const T *row, int64_t first, int64_t vocab) {
+    float x[E];
 #pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (first + i >= 0 && first + i < vocab) row[first + i] = from_f32<T>(c.get(i));   // exact: it was rounded when packed
+    for (int i = 0; i < E; ++i) {
+      x[i] = -INFINITY;
+      if (first + i >= 0 && first + i < vocab) x[i] = to_f32<T>(row[first + i]);
     }
+    c.pack(x);
   }
+  __device__ __forceinline__ void store_some(T *row, int64_t first, int64_t vocab) const {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (first + i >= 0 && first + i < vocab) row[first + i] = from_f32<T>(c.get(i));   // exact: it was rounded when packed
+  }
+  __device__ __forceinline__ float2 pair(int i) const { return make_float2(c.get(2 * i), c.get(2 * i + 1)); }
   __device__ __forceinline__ float largest() const {
-    float m = c.get(0);
-#pragma unroll
-    for (int i = 1; i < E; ++i) m = fmaxf(m, c.get(i));
-    return m;
+    if constexpr (sizeof(T) == 4) {
+      return fmaxf(fmaxf(c.get(0), c.get(1)), fmaxf(c.get(2), c.get(3)));
+    } else {   // maxima of both halves of the words; like fmaxf they pass over a NaN
+      const __nv_bfloat162 *w = reinterpret_cast<const __nv_bfloat162 *>(c.raw.v);
+      const __nv_bfloat162 m = __hmax2(__hmax2(w[0], w[1]), __hmax2(w[2], w[3]));
+      return fmaxf(__low2float(m), __high2float(m));
+    }
   }
-  __device__ __forceinline__ float sum_exp(float m, float scale) const {
-    float l = 0.f;
+  __device__ __forceinline__ float2 sum_exp(float2 l, float base, float scale) const {
 #pragma unroll
-    for (int i = 0; i < E; ++i) l += exp2_approx((c.get(i) - m) * scale);
+    for (int i = 0; i < kPairs; ++i) {
+      const float2 y = exponents(pair(i), base, scale);
+      l = add2(l, make_float2(exp2_approx(y.x), exp2_approx(y.y)));
+    }
     return l;
   }
+  __device__ __forceinline__ void to_gradient(float base, float scale, float c_) {
+    float g[E];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      const float2 y = exponents(pair(i), base, scale);
+      const float2 z = mul2(make_float2(exp2_approx(y.x), exp2_approx(y.y)), make_float2(c_, c_));
+      g[2 * i] = z.x;
+      g[2 * i + 1] = z.y;
+    }
+    c.pack(g);
+  }
+};
+
+// log x to 2^-25 absolutely: the exponent's part in 64 bits, the mantissa's, at most log(2) / 2 in size, by logf.  A log in 64
+// bits takes a warp over a microsecond, which rows of a few microseconds would wait for.
+__device__ __forceinline__ double log_of(float x) {
+  if (!(x >= 1e-37f && x < INFINITY)) return (double)logf(x);
+  const int32_t bits = __float_as_int(x) - 0x3f3504f3;   // 1 / sqrt(2) .. sqrt(2)
+  const int32_t k = bits >> 23;
+  return (double)k * 0.69314718055994531 + (double)logf(__int_as_float((bits & 0x7fffff) + 0x3f3504f3));
+}
+
+// What some of the teacher's entries contribute: their largest logit, the sum of e = exp((top - m) / tau), and the sum of
+// e (top - s) over those whose column is at hand.  The last one is a difference of large terms in the end: 64 bits.
+struct Teacher {
+  float m, sum;
+  double a;
+};
+
+// Resident CTAs of `threads`: 64 registers per thread for the gradient, 48 for the loss
+constexpr int per_sm(int threads, bool grad) { return (grad ? 1024 : 1280) / threads; }
+
+struct __align__(16) Part {   // one CTA's share of a row
+  double a;
+  MaxSum ms;
 };
 
 struct Shared {
-  double a[kMaxWarps], p[kMaxWarps];
   MaxSum ms[kMaxWarps];
-  int32_t id[STAGE_DISTILL_MAX_TOP];    // -1: padding
-  float e[STAGE_DISTILL_MAX_TOP];       // exp((top - max) / tau), to be divided by their sum
+  Teacher teacher[kMaxWarps];
+  Part ctas[2][kMaxCluster];            // rows take turns
+  int32_t id[STAGE_DISTILL_MAX_TOP];    // -1: padding, or another CTA's column
+  float e[STAGE_DISTILL_MAX_TOP];       // relative to the maximum of the warp that has the entry
   float at[STAGE_DISTILL_MAX_TOP];      // the student's logit there
 };
 
-// One CTA per row, which streams through it: once for (m, L), once more for the gradient.
-template <typename T, bool GRAD>
-__global__ void __launch_bounds__(kMaxThreads) distill_stream_kernel(const __grid_constant__ DistillArgs a) {
-  constexpr int E = 16 / (int)sizeof(T), kUnroll = 4;
+// A CTA, or for few rows a cluster of them that shares a row's columns, streams through a row: once for (m, L), once more for
+// the gradient, out of L2.  A row is cut at 16-byte boundaries into pieces: piece i holds the elements from i E - shift on, and
+// only the first and the last piece can reach past the row; they are taken element by element, the others without a check.
+// The teacher's entries, one per thread, are loaded a row ahead and the student's logits at their ids with the row's first
+// pieces, so that their latency passes behind the row.
+template <typename T, int kThreads, bool GRAD>
+__global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kernel(const __grid_constant__ DistillArgs a) {
+  constexpr int E = Piece<T>::E, U = 4, kWarps = kThreads / 32;   // U pieces in flight per thread
   __shared__ Shared sh;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, threads = blockDim.x, warps = threads >> 5;
-  const float scale = kLog2e / a.tau;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  uint32_t cluster, rank;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;\n" : "=r"(cluster));
+  asm volatile("mov.u32 %0, %%cluster_ctarank;\n" : "=r"(rank));
+  const float scale = kLog2e / a.tau, inv_tau = 1.f / a.tau;
+  if (cluster > 1) cluster_sync();   // the peers have started: their shared memory may be written
   pdl_enter();
-  for (int64_t t = blockIdx.x; t < a.n; t += gridDim.x) {
-    const float w = a.weight != nullptr ? a.weight[t] : 1.f;
+  const int64_t workers = gridDim.x / cluster;
+  int turn = 0, next_id = -1;
+  float next_top = 0.f, next_w = 1.f;
+  auto look = [&](int64_t t) {
+    if (t >= a.n) return;
+    if (tid < a.top_k) {
+      next_id = a.ids[t * a.ldi + tid];
+      next_top = a.top[t * a.ldt + tid];
+    }
+    if (a.weight != nullptr) next_w = a.weight[t];
+  };
+  look(blockIdx.x / cluster);
+  for (int64_t t = blockIdx.x / cluster; t < a.n; t += workers) {
     const T *row = static_cast<const T *>(a.logits) + t * a.ldl;
     T *out = GRAD ? static_cast<T *>(a.out) + t * a.ldd : nullptr;
     const int shift = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-    const bool whole = GRAD && ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
-    const int64_t pieces = (shift + a.vocab + E - 1) / E;
+    const int pieces = (int)((shift + a.vocab + E - 1) / E), per = (pieces + (int)cluster - 1) / (int)cluster;
+    const int lo = min((int)rank * per, pieces), hi = min(lo + per, pieces);
+    const int in_lo = max(lo, 1), in_hi = min(hi, pieces - 1);   // without the row's first and last piece
+    // the piece at the row's end that this thread takes, if any: the first one, or the last one where that is another
+    const int edge = tid == 0 && lo == 0 && hi > 0 ? 0 : tid == 32 && hi == pieces && pieces > 1 && lo < hi ? pieces - 1 : -1;
+    const unsigned char *src = reinterpret_cast<const unsigned char *>(row) - shift * (int)sizeof(T) + ((int64_t)in_lo + tid) * 16;
+    unsigned char *dst = GRAD ? reinterpret_cast<unsigned char *>(out) - shift * (int)sizeof(T) + ((int64_t)in_lo + tid) * 16 : nullptr;
+    const bool same = GRAD && ((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
+    const int mine = in_hi - in_lo - tid;   // pieces from this thread's first one on, every kThreads-th is its own
+    const float w = next_w;
 
-    // the teacher's maximum and sum, by every warp for itself
-    const int32_t *ids = a.ids + t * a.ldi;
-    const float *top = a.top + t * a.ldt;
-    float tm = -INFINITY;
+    // the teacher's entries of this thread: j = tid, tid + kThreads, ...
+    __syncthreads();   // the row before this one is done with what is shared
+    float tm = -INFINITY, own_at = 0.f;
     bool any = false;
-    for (int j = lane; j < a.top_k; j += 32) {
-      const int32_t id = ids[j];
-      const float x = top[j];
+    for (int j = tid; j < a.top_k; j += kThreads) {
+      int32_t id = j == tid ? next_id : a.ids[t * a.ldi + j];
+      const float v = j == tid ? next_top : a.top[t * a.ldt + j];
       if (id >= 0 && id < a.vocab) {
-        tm = fmaxf(tm, x);
-        any = any || x != -INFINITY;
-      } else if (id != -1 && warp == 0 && a.dev_status != nullptr) {
-        atomicOr(a.dev_status, SSN_DEV_BAD_ID);
+        tm = fmaxf(tm, v);
+        any = any || v != -INFINITY;
+      } else {
+        if (id != -1 && rank == 0 && a.dev_status != nullptr) atomicOr(a.dev_status, SSN_DEV_BAD_ID);
+        id = -1;
       }
+      const int piece = id >= 0 ? (shift + id) / E : -1;
+      const float s = piece >= lo && piece < hi ? to_f32<T>(row[id]) : 0.f;
+      if (j == tid) own_at = s;   // it arrives while the row passes
+      else sh.at[j] = s;
+      sh.e[j] = id >= 0 ? v : -INFINITY;
+      sh.id[j] = piece >= lo && piece < hi ? id : -1;
     }
-    for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, o));
-    any = __any_sync(0xffffffffu, any);
-    if (w == 0.f || !any) {   // nothing to learn from this row
-      if (tid == 0) a.loss[t] = 0.f;
+    look(t + workers);
+    const bool on = __syncthreads_or(any && w != 0.f);
+    if (!on) {   // nothing to learn from this row
+      if (tid == 0 && rank == 0) a.loss[t] = 0.f;
       if (GRAD) {
-        const float zero[E] = {};
         Piece<T> z;
-        z.c.pack(zero);
-        for (int64_t i = tid; i < pieces; i += threads) z.store(out, i * E - shift, a.vocab, whole);
+        z.set(0.f);
+        if (same)
+          for (int i = 0; i < mine; i += kThreads) z.store(dst + (int64_t)i * 16);
+        else
+          for (int i = 0; i < mine; i += kThreads) z.store_some(out, (int64_t)(in_lo + tid + i) * E - shift, a.vocab);
+        if (edge >= 0) z.store_some(out, (int64_t)edge * E - shift, a.vocab);
       }
       continue;
     }
-    const float inv_tau = 1.f / a.tau;
-    float tsum = 0.f;
-    for (int j = lane; j < a.top_k; j += 32) {
-      const int32_t id = ids[j];
-      if (id >= 0 && id < a.vocab) tsum += expf((top[j] - tm) * inv_tau);
-    }
-    for (int o = 16; o > 0; o >>= 1) tsum += __shfl_xor_sync(0xffffffffu, tsum, o);
-    __syncthreads();   // the row before this one is done with what is shared
-    double part_a = 0.0, part_p = 0.0;   // sum p (log p - x), sum p
-    for (int j = tid; j < a.top_k; j += threads) {
-      int32_t id = ids[j];
-      if (id < 0 || id >= a.vocab) id = -1;
-      float e = 0.f, at = 0.f;
-      if (id >= 0) {
-        at = to_f32<T>(row[id]);
-        e = expf((top[j] - tm) * inv_tau);
-        const float p = e / tsum;
-        if (!(p == 0.f)) {
-          part_a += (double)p * (((double)top[j] - (double)tm - (double)at) / (double)a.tau - log((double)tsum));
-          part_p += (double)p;
-        }
-      }
-      sh.id[j] = id;
-      sh.e[j] = e;
-      sh.at[j] = at;
-    }
 
-    MaxSum ms{-INFINITY, 0.f};
-    for (int64_t i0 = tid; i0 < pieces; i0 += (int64_t)threads * kUnroll) {
-      Piece<T> x[kUnroll];
-      float m = ms.m;
+    float m = -INFINITY;
+    float2 l = make_float2(0.f, 0.f);
+    auto add = [&](Piece<T> (&x)[U]) {
+      float most = m;
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) x[u].load(row, (i0 + (int64_t)u * threads) * E - shift, a.vocab);
+      for (int u = 0; u < U; ++u) most = fmaxf(most, x[u].largest());
+      const float base = base_of(most), f = rescale(m, base, scale);
+      l = mul2(l, make_float2(f, f));
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) m = fmaxf(m, x[u].largest());
-      const float at = m == -INFINITY ? 0.f : m;
-      float l = ms.l * exp2_approx((ms.m - at) * scale);
+      for (int u = 0; u < U; ++u) l = x[u].sum_exp(l, base, scale);
+      m = most;
+    };
+    Piece<T> x[U];
+    int at = 0;
+    for (; at + (U - 1) * kThreads < mine; at += U * kThreads) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u) l += x[u].sum_exp(at, scale);
-      ms = {m, l};
+      for (int u = 0; u < U; ++u) x[u].load(src + (int64_t)(at + u * kThreads) * 16, !GRAD);
+      add(x);
     }
-    for (int o = 16; o > 0; o >>= 1) {
-      const MaxSum other{__shfl_xor_sync(0xffffffffu, ms.m, o), __shfl_xor_sync(0xffffffffu, ms.l, o)};
-      ms = lane & o ? merge(other, ms, scale) : merge(ms, other, scale);
-      part_a += __shfl_xor_sync(0xffffffffu, part_a, o);
-      part_p += __shfl_xor_sync(0xffffffffu, part_p, o);
+    if (at < mine || edge >= 0) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (u < U - 1 && at + u * kThreads < mine) x[u].load(src + (int64_t)(at + u * kThreads) * 16, !GRAD);
+        else x[u].set(-INFINITY);
+      }
+      if (edge >= 0) x[U - 1].load_some(row, (int64_t)edge * E - shift, a.vocab);
+      add(x);
     }
-    if (lane == 0) {
-      sh.ms[warp] = ms;
-      sh.a[warp] = part_a;
-      sh.p[warp] = part_p;
+    const MaxSum own = merge_warp({m, l.x + l.y}, scale);
+    if (lane == 0) sh.ms[warp] = own;
+    if (warp * 32 < a.top_k) {   // the warp's entries
+      if (tid < a.top_k) sh.at[tid] = own_at;
+      for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, o));
+      float sum = 0.f;
+      double sa = 0.0;
+      for (int j = tid; j < a.top_k; j += kThreads) {
+        const float v = sh.e[j];
+        float e = 0.f;
+        if (v != -INFINITY) {   // of an entry, and one with mass
+          e = expf((v - tm) * inv_tau);
+          if (sh.id[j] >= 0 && !(e == 0.f)) sa += (double)e * ((double)v - (double)sh.at[j]);
+        }
+        sum += e;
+        sh.e[j] = e;
+      }
+      for (int o = 16; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        sa += __shfl_xor_sync(0xffffffffu, sa, o);
+      }
+      if (lane == 0) sh.teacher[warp] = {tm, sum, sa};
     }
     __syncthreads();
-    ms = sh.ms[0];
-    for (int i = 1; i < warps; ++i) ms = merge(ms, sh.ms[i], scale);
-    if (tid == 0) {
-      double sa = 0.0, sp = 0.0;
-      for (int i = 0; i < warps; ++i) sa += sh.a[i], sp += sh.p[i];
-      const double lse = (double)ms.m / (double)a.tau + log((double)ms.l);
-      a.loss[t] = (float)((double)w * (double)a.tau * (double)a.tau * (sa + sp * lse));
+    MaxSum ms = merge_warp(lane < kWarps ? sh.ms[lane] : MaxSum{-INFINITY, 0.f}, scale);
+    // the teacher's row: the warps' shares, one after the other
+    const int tw = min(kWarps, (a.top_k + 31) / 32);
+    float top_m = sh.teacher[0].m, tsum = 0.f;
+    double ta = 0.0;
+    for (int i = 1; i < tw; ++i) top_m = fmaxf(top_m, sh.teacher[i].m);
+    auto share = [&](int i) { return sh.teacher[i].m == -INFINITY ? 0.f : expf((sh.teacher[i].m - top_m) * inv_tau); };
+    for (int i = 0; i < tw; ++i) {
+      const float f = share(i);
+      tsum += sh.teacher[i].sum * f;
+      ta += sh.teacher[i].a * (double)f;
+    }
+    if (cluster > 1) {
+      if (warp == 0) {
+        if (lane < (int)cluster) {   // to the CTA of that rank
+          const uint32_t to = map_to_rank(smem_address(&sh.ctas[turn][rank]), (uint32_t)lane);
+          asm volatile("st.shared::cluster.f64 [%0], %1;\n" ::"r"(to), "d"(ta) : "memory");
+          asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};\n" ::"r"(to + 8), "f"(ms.m), "f"(ms.l) : "memory");
+        }
+        __syncwarp();
+      }
+      cluster_sync();
+      ms = merge_warp(lane < (int)cluster ? sh.ctas[turn][lane].ms : MaxSum{-INFINITY, 0.f}, scale);
+      ta = 0.0;
+      for (int i = 0; i < (int)cluster; ++i) ta += sh.ctas[turn][i].a;
+      turn ^= 1;
+    }
+    if (tid == 0 && rank == 0) {
+      // log p = (top - top_m) / tau - log tsum, the student's log sum is m / tau + log l
+      const double tau = (double)a.tau;
+      const double r0 = (double)(1.f / tsum), r1 = r0 * (2.0 - (double)tsum * r0);   // 1 / tsum: a division in 64 bits takes long
+      a.loss[t] = (float)((double)w * tau * (ta * r1 - (double)top_m + (double)ms.m + tau * (log_of(ms.l) - log_of(tsum))));
     }
     if (GRAD) {
       const float c = w * a.tau / ms.l;
-      for (int64_t i = tid; i < pieces; i += threads) {
-        Piece<T> x;
-        x.load(row, i * E - shift, a.vocab);
-        float g[E];
+      auto put = [&](Piece<T> &v, int i) {
+        v.to_gradient(ms.m, scale, c);
+        if (same) v.store(dst + (int64_t)i * 16);
+        else v.store_some(out, (int64_t)(in_lo + tid + i) * E - shift, a.vocab);
+      };
+      // from the end: what was read last is what L2 has for certain
+      at = mine > 0 ? (mine - 1) / kThreads * kThreads : -1;
+      for (; at - (U - 1) * kThreads >= 0; at -= U * kThreads) {
 #pragma unroll
-        for (int q = 0; q < E; ++q) g[q] = exp2_approx((x.c.get(q) - ms.m) * scale) * c;
-        x.c.pack(g);
-        x.store(out, i * E - shift, a.vocab, whole);
+        for (int u = 0; u < U; ++u) x[u].load(src + (int64_t)(at - u * kThreads) * 16, true);
+#pragma unroll
+        for (int u = 0; u < U; ++u) put(x[u], at - u * kThreads);
+      }
+      for (; at >= 0; at -= kThreads) {
+        x[0].load(src + (int64_t)at * 16, true);
+        put(x[0], at);
+      }
+      if (edge >= 0) {
+        x[0].load_some(row, (int64_t)edge * E - shift, a.vocab);
+        x[0].to_gradient(ms.m, scale, c);
+        x[0].store_some(out, (int64_t)edge * E - shift, a.vocab);
       }
       __syncthreads();   // the teacher's ids are written a second time, after the row
-      for (int j = tid; j < a.top_k; j += threads) {
-        const int32_t id = sh.id[j];
-        if (id < 0) continue;
+      // by the first entry of an id, with the p of all of them: eight lanes look through the entries for one
+      for (int j = tid >> 3; j < (a.top_k + 3 & ~3); j += kThreads / 8) {
+        const int32_t id = j < a.top_k ? sh.id[j] : -1;
         float p = 0.f;
         bool first = true;
-        for (int i = 0; i < a.top_k; ++i)
-          if (sh.id[i] == id) {
-            first = first && i >= j;
-            p += sh.e[i];
-          }
-        if (first) out[id] = from_f32<T>(exp2_approx((sh.at[j] - ms.m) * scale) * c - w * a.tau * (p / tsum));
+        if (id >= 0)
+          for (int i = tid & 7; i < a.top_k; i += 8)
+            if (sh.id[i] == id) {
+              first = first && i >= j;
+              p += sh.e[i] * share((i % kThreads) / 32);
+            }
+        for (int o = 4; o > 0; o >>= 1) {
+          p += __shfl_xor_sync(0xffffffffu, p, o);
+          first = __shfl_xor_sync(0xffffffffu, (int)first, o) != 0 && first;
+        }
+        if ((tid & 7) == 0 && id >= 0 && first) out[id] = from_f32<T>(exp2_approx((sh.at[j] - ms.m) * scale) * c - w * a.tau * (p / tsum));
       }
     }
   }
 }
 
-template <typename T>
-cudaError_t launch_distill(const DistillArgs &a, cudaStream_t stream) {
-  const int64_t cap = (int64_t)stage_sm_count() * 4;
-  const unsigned grid = (unsigned)(a.n < cap ? a.n : cap);
-  if (a.out != nullptr) return launch_dependent(distill_stream_kernel<T, true>, grid, kMaxThreads, 0, stream, 1, a);
-  return launch_dependent(distill_stream_kernel<T, false>, grid, kMaxThreads, 0, stream, 1, a);
+template <typename T, int kThreads, bool GRAD> cudaError_t launch_threads(const DistillArgs &a, cudaStream_t stream) {
+  const int sms = stage_sm_count();
+  const int64_t cap = (int64_t)sms * per_sm(kThreads, GRAD);
+  int cluster = 1;   // CTAs per row, while there are SMs without one and pieces enough for it
+  while (cluster < kMaxCluster && a.n * cluster <= sms && a.vocab / (Piece<T>::E * cluster * 2) >= 2 * kThreads) cluster *= 2;
+  const int64_t workers = a.n < cap / cluster ? a.n : cap / cluster;
+  return launch_dependent(distill_kernel<T, kThreads, GRAD>, (unsigned)(workers * cluster), kThreads, 0, stream, cluster, a);
+}
+
+// Threads per CTA by the row's bytes: a row costs a CTA a few microseconds besides its bytes, which more CTAs per SM hide, while
+// long rows want fewer of them (the second pass finds its row in L2).  0.5 GB of logits in rows of 64 / 130 / 256 KB, with the
+// gradient: 128 threads 254 / 276 / 292 us, 256 threads 287 / 246 / 269; the loss alone 104 / 103 / 109 and 130 / 104 / 101.
+// 512 threads would take the longest rows' gradient in 245, but the loss alone in 113; both calls add a row up in the same
+// order, so that its loss is the same number with the gradient and without.
+template <typename T> cudaError_t launch_distill(const DistillArgs &a, cudaStream_t stream) {
+  const bool many = a.vocab * (int64_t)sizeof(T) >= 98304;
+  if (a.out == nullptr) return many ? launch_threads<T, 256, false>(a, stream) : launch_threads<T, 128, false>(a, stream);
+  return many ? launch_threads<T, 256, true>(a, stream) : launch_threads<T, 128, true>(a, stream);
 }
 
 }  // namespace

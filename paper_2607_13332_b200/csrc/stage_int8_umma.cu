@@ -57,10 +57,13 @@ template <typename T> cudaError_t launch_typed(const Int8Matmul &m, int sms, cud
 
 }  // namespace
 
-cudaError_t launch_int8_umma(const Int8Matmul &m, bool f32, int sm_count, cudaStream_t stream) {
+cudaError_t launch_int8_umma(const Int8Matmul &given, bool f32, int sm_count, cudaStream_t stream) {
+  Int8Matmul m = given;   // the pitch of a single row does not matter
+  if (m.n == 1) m.ldx = (m.inner + 15) / 16 * 16;
+  if (m.outer == 1) m.ldw = (m.inner + 15) / 16 * 16;
   if (((reinterpret_cast<uintptr_t>(m.xq) | reinterpret_cast<uintptr_t>(m.wq) | (uintptr_t)m.ldx | (uintptr_t)m.ldw) & 15) != 0)
     return cudaErrorNotSupported;
-  // row coordinates and strides a tensor map can hold (a single row has no stride that matters)
+  // row coordinates and strides a tensor map can hold
   constexpr int64_t kRows = 0x7fffff00, kPitch = (int64_t)1 << 40;
   if (m.n > kRows || m.outer > kRows || m.ldx >= kPitch || m.ldw >= kPitch || sm_count < 2) return cudaErrorNotSupported;
   return f32 ? launch_typed<float>(m, sm_count, stream) : launch_typed<__nv_bfloat16>(m, sm_count, stream);

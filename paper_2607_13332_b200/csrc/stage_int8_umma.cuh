@@ -76,15 +76,6 @@ template <int CG> __device__ __forceinline__ void int8_commit(uint32_t bar) {
   else
     umma_commit(bar);
 }
-__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, uint32_t rank) {
-  uint32_t remote;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;\n" : "=r"(remote) : "r"(addr), "r"(rank));
-  return remote;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;\n" ::: "memory");
-}
-
 template <int CG, int BN, bool SWAP, typename T>
 __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
   using Cfg = Int8Config<CG, BN, SWAP>;

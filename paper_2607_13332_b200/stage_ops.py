@@ -14,23 +14,28 @@ from .runner import _TORCH_DTYPE, _ld, _ptr, _stream
 _lib = binding.library()
 _CODES = {torch.float32: binding.SSN_F32, torch.bfloat16: binding.SSN_BF16}
 
+# Calls of one token are shorter on the GPU than on the host, so every call asks each tensor once for its type, device, shape
+# and strides, and makes its outputs with the cheapest allocation there is: (shape, strides, type) on the current device, 0.9 us
+# against 1.8 to 3.5 us for torch.empty.
+_current_device = torch._C._cuda_getDevice
+_new = torch._C._dynamo.guards._empty_strided_cuda
+
 
 def _here(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:
     """t, if it is a tensor of that type on the current device (the one whose stream the kernels are put on)."""
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+    if t.get_device() != _current_device():     # -1 for a tensor on the host
         raise ValueError(f"{what}: expected a CUDA tensor on the current device")
     if t.dtype != dtype:
         raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
     return t
 
 
-def _ints(t: Optional[torch.Tensor], n: int, what: str) -> int:
-    """Address of n contiguous int32, or 0."""
+def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) -> int:
+    """Address of n contiguous values of that type, or 0."""
     if t is None:
         return 0
-    _here(t, torch.int32, what)
-    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{what}: expected {n} contiguous int32")
+    if _here(t, dtype, what).shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{what}: expected {n} contiguous values")
     return t.data_ptr()
 
 
@@ -59,6 +64,7 @@ class QKNormRope:
         self.dev_status = torch.zeros(1, dtype=torch.int32, device=device)
         self.c = binding.make_qk_rope(head_dim, rot, binding.DTYPES[dtype], binding.PAIRINGS[pairing], eps, _ptr(wq), _ptr(wk),
                                       _ptr(table), _ld(table) if table is not None else 0, max_pos, self.dev_status.data_ptr())
+        self._ref = byref(self.c)
 
     def take_status(self) -> int:
         """Read and clear the device status word (synchronises): SSN_DEV_BAD_POS of every call since the last read."""
@@ -72,21 +78,32 @@ class QKNormRope:
             if n * heads:
                 raise ValueError(f"{what} is missing")
             return 0, 0, 0
-        if t.dtype != self.dtype or t.get_device() != torch._C._cuda_getDevice():
+        if t.dtype != self.dtype or t.get_device() != _current_device():
             raise ValueError(f"{what}: expected {self.dtype} on the current device")
-        st = t.stride()
-        if t.shape != (n, heads, self.head_dim) or st[2] != 1:
-            raise ValueError(f"{what}: expected [{n}, {heads}, {self.head_dim}] with unit stride along the last dimension")
-        return t.data_ptr(), st[0], st[1]
+        if t.shape != (n, heads, self.head_dim):
+            raise ValueError(f"{what}: expected [{n}, {heads}, {self.head_dim}]")
+        token, head, unit = t.stride()
+        if unit != 1:
+            raise ValueError(f"{what}: expected unit stride along the last dimension")
+        return t.data_ptr(), token, head
 
-    def _empty(self, like: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
-        return None if like is None else torch.empty(like.shape, dtype=self.dtype, device=like.device)
+    def _out(self, t: Optional[torch.Tensor], n: int, heads: int, absent: bool, what: str):
+        """The output tensor, made here unless it is given, and its (address, token stride, head stride)."""
+        if t is not None:
+            return t, self._heads(t, n, heads, what)
+        if absent:
+            return None, (0, 0, 0)
+        d = self.head_dim
+        t = _new((n, heads, d), (heads * d, d, 1), self.dtype)
+        return t, (t.data_ptr(), heads * d, d)
 
     @staticmethod
     def _sizes(q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> Tuple[int, int, int]:
         some = q if q is not None else k
         if some is None:
             raise ValueError("neither queries nor keys")
+        if some.dim() != 3:
+            raise ValueError("expected [tokens, heads, head_dim]")
         return some.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
 
     def forward(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Optional[torch.Tensor] = None, seq_len: int = 0,
@@ -94,14 +111,13 @@ class QKNormRope:
         """q [n, q_heads, head_dim] and k [n, k_heads, head_dim] (views of any strides; either may be None), normed and rotated.
         Positions: pos int32[n], or t mod seq_len.  An output given may be its input.  Returns (q_out, k_out)."""
         n, qh, kh = self._sizes(q, k)
-        if q_out is None:
-            q_out = self._empty(q)
-        if k_out is None:
-            k_out = self._empty(k)
-        st = _lib.stage_qk_rope_forward(byref(self.c), *self._heads(q, n, qh, "q"), qh, *self._heads(k, n, kh, "k"), kh,
-                                        *self._heads(q_out, n, qh, "q_out"), *self._heads(k_out, n, kh, "k_out"),
-                                        _ints(pos, n, "pos"), n, seq_len, _stream())
-        binding.check(st, "stage_qk_rope_forward")
+        qa, ka = self._heads(q, n, qh, "q"), self._heads(k, n, kh, "k")
+        q_out, qo = self._out(q_out, n, qh, q is None, "q_out")
+        k_out, ko = self._out(k_out, n, kh, k is None, "k_out")
+        st = _lib.stage_qk_rope_forward(self._ref, *qa, qh, *ka, kh, *qo, *ko, _vector(pos, n, torch.int32, "pos"), n, seq_len,
+                                        _stream())
+        if st:
+            binding.check(st, "stage_qk_rope_forward")
         return q_out, k_out
 
     def backward(self, dq: Optional[torch.Tensor], dk: Optional[torch.Tensor], q: Optional[torch.Tensor], k: Optional[torch.Tensor],
@@ -110,45 +126,44 @@ class QKNormRope:
         """From the gradients of forward's outputs and forward's inputs: (dq_in, dk_in, dwq, dwk), the gains' gradients in
         fp32 [head_dim], or None without `gains`.  dq_in may be dq, dk_in dk."""
         n, qh, kh = self._sizes(q, k)
-        if dq_in is None:
-            dq_in = self._empty(q)
-        if dk_in is None:
-            dk_in = self._empty(k)
-        some = q if q is not None else k
-        dwq = dwk = None
-        ws, nbytes = 0, 0
+        dqa, dka = self._heads(dq, n, qh, "dq"), self._heads(dk, n, kh, "dk")
+        qa, ka = self._heads(q, n, qh, "q"), self._heads(k, n, kh, "k")
+        dq_in, dqo = self._out(dq_in, n, qh, q is None, "dq_in")
+        dk_in, dko = self._out(dk_in, n, kh, k is None, "dk_in")
+        dwq = dwk = scratch = None
+        nbytes = 0
         if gains:
-            nbytes = _lib.stage_qk_rope_workspace_bytes(byref(self.c), n, qh, kh)
-            dw = torch.empty((2, self.head_dim), dtype=torch.float32, device=some.device)
-            dwq, dwk = dw[0], dw[1]
-            scratch = torch.empty(nbytes, dtype=torch.uint8, device=some.device)
-            ws = scratch.data_ptr()
-        st = _lib.stage_qk_rope_backward(byref(self.c), *self._heads(dq, n, qh, "dq"), *self._heads(dk, n, kh, "dk"),
-                                         *self._heads(q, n, qh, "q"), qh, *self._heads(k, n, kh, "k"), kh,
-                                         *self._heads(dq_in, n, qh, "dq_in"), *self._heads(dk_in, n, kh, "dk_in"), _ptr(dwq),
-                                         _ptr(dwk), _ints(pos, n, "pos"), n, seq_len, ws, nbytes, _stream())
-        binding.check(st, "stage_qk_rope_backward")
+            d = self.head_dim
+            nbytes = _lib.stage_qk_rope_workspace_bytes(self._ref, n, qh, kh)
+            dwq, dwk = _new((d,), (1,), torch.float32), _new((d,), (1,), torch.float32)
+            scratch = _new((nbytes,), (1,), torch.uint8)      # one per call: captured calls share none
+        st = _lib.stage_qk_rope_backward(self._ref, *dqa, *dka, *qa, qh, *ka, kh, *dqo, *dko, _ptr(dwq), _ptr(dwk),
+                                         _vector(pos, n, torch.int32, "pos"), n, seq_len, _ptr(scratch), nbytes, _stream())
+        if st:
+            binding.check(st, "stage_qk_rope_backward")
         return dq_in, dk_in, dwq, dwk
 
 
 # ---- loss against a teacher's top logits --------------------------------------------------------------------------------------
 def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight: Optional[torch.Tensor], temperature: float,
              dlogits: Optional[torch.Tensor], dev_status: Optional[torch.Tensor]) -> torch.Tensor:
-    if logits.dtype not in _CODES:
+    code = _CODES.get(logits.dtype)
+    if code is None:
         raise ValueError("logits: expected fp32 or bf16")
     n, vocab = _here(logits, logits.dtype, "logits").shape
     if _here(ids, torch.int32, "ids").shape != _here(top, torch.float32, "top").shape or ids.dim() != 2 or ids.shape[0] != n:
         raise ValueError(f"ids, top: expected [{n}, top_k] each")
-    if weight is not None and (_here(weight, torch.float32, "weight").shape != (n,) or not weight.is_contiguous()):
-        raise ValueError(f"weight: expected {n} contiguous fp32")
-    if dlogits is not None and _here(dlogits, logits.dtype, "dlogits").shape != logits.shape:
-        raise ValueError("dlogits: expected the shape of the logits")
-    _ints(dev_status, 1, "dev_status")
-    loss = torch.empty(n, dtype=torch.float32, device=logits.device)
-    st = _lib.stage_distill_loss(logits.data_ptr(), _ld(logits), _CODES[logits.dtype], n, vocab, ids.data_ptr(), _ld(ids),
-                                 top.data_ptr(), _ld(top), ids.shape[1], _ptr(weight), temperature, loss.data_ptr(), _ptr(dlogits),
-                                 _ld(dlogits) if dlogits is not None else 0, _ptr(dev_status), _stream())
-    binding.check(st, "stage_distill_loss")
+    out, ldd = 0, 0
+    if dlogits is not None:
+        if _here(dlogits, logits.dtype, "dlogits").shape != logits.shape:
+            raise ValueError("dlogits: expected the shape of the logits")
+        out, ldd = dlogits.data_ptr(), _ld(dlogits)
+    loss = _new((n,), (1,), torch.float32)
+    st = _lib.stage_distill_loss(logits.data_ptr(), _ld(logits), code, n, vocab, ids.data_ptr(), _ld(ids), top.data_ptr(), _ld(top),
+                                 ids.shape[1], _vector(weight, n, torch.float32, "weight"), temperature, loss.data_ptr(), out, ldd,
+                                 _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
+    if st:
+        binding.check(st, "stage_distill_loss")
     return loss
 
 
@@ -164,8 +179,8 @@ def distill_loss_grad(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor
     """distill_loss and the gradient of its sum with respect to the logits, in one pass: (loss, dlogits).  dlogits may be the
     logits; made here, it has the logits' leading dimension."""
     if dlogits is None:
-        n, vocab = logits.shape
-        dlogits = torch.empty((n, max(_ld(logits), vocab)), dtype=logits.dtype, device=logits.device)[:, :vocab]
+        ld = _ld(_here(logits, logits.dtype, "logits"))
+        dlogits = _new(tuple(logits.shape), (ld, 1), logits.dtype)
     return _distill(logits, ids, top, weight, temperature, dlogits, dev_status), dlogits
 
 
@@ -173,18 +188,21 @@ def distill_loss_grad(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor
 def int8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None):
     """(q, scale): the rows of x (fp32 or bf16) in 8 bits with one fp32 scale each.  q made here has a leading dimension that
     is a multiple of 16, which is what int8_matmul's TMA kernels need."""
-    if x.dtype not in _CODES:
+    code = _CODES.get(x.dtype)
+    if code is None:
         raise ValueError("x: expected fp32 or bf16")
     rows, cols = _here(x, x.dtype, "x").shape
     if q is None:
-        q = torch.empty((rows, -(-cols // 16) * 16), dtype=torch.int8, device=x.device)
-        if q.shape[1] != cols:
-            q = q[:, :cols]
+        ldq = -(-cols // 16) * 16
+        q = _new((rows, cols), (ldq, 1), torch.int8)
     elif _here(q, torch.int8, "q").shape != x.shape:
         raise ValueError("q: expected the shape of x")
-    scale = torch.empty(rows, dtype=torch.float32, device=x.device)
-    st = _lib.stage_int8_quantize(x.data_ptr(), _ld(x), _CODES[x.dtype], rows, cols, q.data_ptr(), _ld(q), scale.data_ptr(), _stream())
-    binding.check(st, "stage_int8_quantize")
+    else:
+        ldq = _ld(q)
+    scale = _new((rows,), (1,), torch.float32)
+    st = _lib.stage_int8_quantize(x.data_ptr(), _ld(x), code, rows, cols, q.data_ptr(), ldq, scale.data_ptr(), _stream())
+    if st:
+        binding.check(st, "stage_int8_quantize")
     return q, scale
 
 
@@ -192,18 +210,18 @@ def int8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.
                 out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [n, outer] of dtype = (xq [n, inner] times wq [outer, inner] transposed), scaled by xs [n] and ws [outer]."""
     n, inner = _here(xq, torch.int8, "xq").shape
-    outer = _here(wq, torch.int8, "wq").shape[0]
-    if wq.shape[1] != inner:
+    outer, depth = _here(wq, torch.int8, "wq").shape
+    if depth != inner:
         raise ValueError(f"wq: expected [outer, {inner}]")
-    for s, rows, what in ((xs, n, "xs"), (ws, outer, "ws")):
-        if _here(s, torch.float32, what).shape != (rows,) or not s.is_contiguous():
-            raise ValueError(f"{what}: expected {rows} contiguous fp32")
     if out is None:
-        out = torch.empty((n, outer), dtype=_TORCH_DTYPE[dtype], device=xq.device)
+        out, ldy = _new((n, outer), (outer, 1), _TORCH_DTYPE[dtype]), outer
     elif _here(out, _TORCH_DTYPE[dtype], "out").shape != (n, outer):
         raise ValueError(f"out: expected [{n}, {outer}]")
-    _ints(dev_status, 1, "dev_status")
-    st = _lib.stage_int8_matmul(xq.data_ptr(), _ld(xq), xs.data_ptr(), wq.data_ptr(), _ld(wq), ws.data_ptr(), n, inner, outer,
-                                out.data_ptr(), _ld(out), binding.DTYPES[dtype], _ptr(dev_status), _stream())
-    binding.check(st, "stage_int8_matmul")
+    else:
+        ldy = _ld(out)
+    st = _lib.stage_int8_matmul(xq.data_ptr(), _ld(xq), _vector(xs, n, torch.float32, "xs"), wq.data_ptr(), _ld(wq),
+                                _vector(ws, outer, torch.float32, "ws"), n, inner, outer, out.data_ptr(), ldy, binding.DTYPES[dtype],
+                                _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
+    if st:
+        binding.check(st, "stage_int8_matmul")
     return out
