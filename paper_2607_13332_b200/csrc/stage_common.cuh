@@ -93,6 +93,74 @@ template <typename T, int V> __device__ __forceinline__ void Chunk<T, V>::pack(c
   }
 }
 
+// Two fp32 values per instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+
+// V values at a time, two per instruction where V is even: d = a b, d = a b + c, d = s a, d = s a + c
+template <int V> __device__ __forceinline__ void v_mul(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
+#pragma unroll
+  for (int i = 0; i + 1 < V; i += 2) {
+    const float2 r = mul2({a[i], a[i + 1]}, {b[i], b[i + 1]});
+    d[i] = r.x, d[i + 1] = r.y;
+  }
+  if constexpr (V == 1) d[0] = a[0] * b[0];
+}
+template <int V> __device__ __forceinline__ void v_fma(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
+#pragma unroll
+  for (int i = 0; i + 1 < V; i += 2) {
+    const float2 r = fma2({a[i], a[i + 1]}, {b[i], b[i + 1]}, {c[i], c[i + 1]});
+    d[i] = r.x, d[i + 1] = r.y;
+  }
+  if constexpr (V == 1) d[0] = fmaf(a[0], b[0], c[0]);
+}
+template <int V> __device__ __forceinline__ void v_scale(float (&d)[V], float s, const float (&a)[V]) {
+#pragma unroll
+  for (int i = 0; i + 1 < V; i += 2) {
+    const float2 r = mul2({s, s}, {a[i], a[i + 1]});
+    d[i] = r.x, d[i + 1] = r.y;
+  }
+  if constexpr (V == 1) d[0] = s * a[0];
+}
+template <int V> __device__ __forceinline__ void v_axpy(float (&d)[V], float s, const float (&a)[V], const float (&c)[V]) {
+#pragma unroll
+  for (int i = 0; i + 1 < V; i += 2) {
+    const float2 r = fma2({s, s}, {a[i], a[i + 1]}, {c[i], c[i + 1]});
+    d[i] = r.x, d[i + 1] = r.y;
+  }
+  if constexpr (V == 1) d[0] = fmaf(s, a[0], c[0]);
+}
+
+template <int V> __device__ __forceinline__ float v_total(const float (&a)[V]) {
+  if constexpr (V == 1) return a[0];
+  else if constexpr (V == 2) return a[0] + a[1];
+  else {
+    float h[V / 2];
+#pragma unroll
+    for (int i = 0; i < V / 2; i += 2) {
+      const float2 r = add2({a[i], a[i + 1]}, {a[i + V / 2], a[i + 1 + V / 2]});
+      h[i] = r.x, h[i + 1] = r.y;
+    }
+    return v_total<V / 2>(h);
+  }
+}
+
 // V floats of a 16-byte aligned (V >= 4) or V * 4-byte aligned table row
 template <int V> __device__ __forceinline__ void load_floats(const float *p, float (&x)[V]) {
   if constexpr (V >= 4) {

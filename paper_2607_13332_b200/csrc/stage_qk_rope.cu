@@ -1,14 +1,16 @@
 // Query/key norm with rotary positions (include/agora_stage.h), forward and backward.
 //
 // A row is one head of one token: D values, one mean of squares, one pass.  Both directions move two (three) rows of D per
-// row and compute a few operations per value, so HBM bounds them; what matters is wide loads, enough of them in flight and
-// no second read.
+// row and compute a few operations per value: HBM bounds the forward pass (65536 tokens x 40 heads of 128 bf16 in 224 us,
+// 6.0 TB/s, 0.92 of a copy), the instructions the gradients (32768 tokens in 215 us, 4.7 TB/s: 426 per warp and four rows, two
+// of three issue slots).
 //
 // A row belongs to a group of G lanes (a power of two).  A lane's unit is V column PAIRS, so that no shuffle moves values:
 // for halves one 16-byte piece at column i and one at i + rot_dim / 2, for adjacent pairs two pieces in a row.  The columns
 // past rot_dim are paired in the same way (i with i + (D - rot_dim) / 2) and pass the rotation untouched.  A warp keeps the
 // table row of its token in registers and goes through the token's heads, 32 / G at a time; blocks are dealt to the query
-// and the key side by their numbers of heads, so that a warp needs one gain (and one gradient of it) only.
+// and the key side by their numbers of heads, so that a warp needs one gain (and one gradient of it) only.  Rows are loaded
+// through a ring in shared memory: loads into registers, as many as fit, left the forward pass at 259 us.
 #include "stage_common.cuh"
 
 #include <cmath>
@@ -17,7 +19,10 @@ namespace ssn {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kBlocksPerSm = 4;
+// Resident blocks, and passes of rows on their way per warp.  65536 x 40 heads of 128 bf16 forward: two blocks four or six passes
+// ahead 224 us, three blocks spill (365).  The gradients of 32768: two to four passes ahead 211-216 us.
+constexpr int kPerSm = 2;
+constexpr int kForwardAhead = 4, kBackAhead = 3;
 
 struct RopeSide {
   const void *x, *dy;   // forward input; incoming gradient (backward)
@@ -37,6 +42,7 @@ struct RopeArgs {
   int32_t *dev_status;
   int64_t n;
   int32_t d, rot, max_pos, seq_len, group_log2;
+  int32_t table_bytes, wide_table;   // a table row's room in shared memory; its rows are on 16-byte boundaries
   float eps;
 };
 
@@ -49,34 +55,66 @@ __device__ __forceinline__ int32_t table_row(const RopeArgs &a, int64_t t) {
   return -1;
 }
 
-// The V pairs of a unit turned by the angle (sign = 1) or back (sign = -1).  lo and hi hold the unit's two pieces.
-template <int V, bool ADJ>
-__device__ __forceinline__ void turn(float (&lo)[V], float (&hi)[V], const float (&c)[V], const float (&s)[V], float sign) {
-  if constexpr (!ADJ) {
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float a = lo[i], b = hi[i], ss = sign * s[i];
-      lo[i] = a * c[i] - b * ss;
-      hi[i] = b * c[i] + a * ss;
-    }
-  } else {
-    float z[2 * V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) z[i] = lo[i], z[V + i] = hi[i];
-#pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float a = z[2 * i], b = z[2 * i + 1], ss = sign * s[i];
-      z[2 * i] = a * c[i] - b * ss;
-      z[2 * i + 1] = b * c[i] + a * ss;
-    }
-#pragma unroll
-    for (int i = 0; i < V; ++i) lo[i] = z[i], hi[i] = z[V + i];
+// V column pairs (a, b) in two pieces of V elements: the halves' pieces are the a and the b, adjacent pairs alternate
+template <typename T, int V, bool ADJ> struct Unit {
+  Chunk<T, V> p0, p1;
+  __device__ __forceinline__ void load(const T *x, int at0, int at1) {
+    p0.load(x + at0);
+    p1.load(x + at1);
   }
+  __device__ __forceinline__ void store(T *x, int at0, int at1) const {
+    p0.store(x + at0);
+    p1.store(x + at1);
+  }
+  // from this lane's place in a ring: the 32 lanes' first pieces, then their second ones
+  __device__ __forceinline__ void take(const unsigned char *place) {
+    p0.load(reinterpret_cast<const T *>(place));
+    p1.load(reinterpret_cast<const T *>(place + 32 * V * sizeof(T)));
+  }
+  __device__ __forceinline__ void get(float (&a)[V], float (&b)[V]) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      a[i] = !ADJ ? p0.get(i) : 2 * i < V ? p0.get(2 * i < V ? 2 * i : 0) : p1.get(2 * i < V ? 0 : 2 * i - V);
+      b[i] = !ADJ ? p1.get(i) : 2 * i + 1 < V ? p0.get(2 * i + 1 < V ? 2 * i + 1 : 0) : p1.get(2 * i + 1 < V ? 0 : 2 * i + 1 - V);
+    }
+  }
+  __device__ __forceinline__ void pack(const float (&a)[V], const float (&b)[V]) {
+    if constexpr (!ADJ) {
+      p0.pack(a);
+      p1.pack(b);
+    } else {
+      float z0[V], z1[V];
+#pragma unroll
+      for (int i = 0; i < 2 * V; ++i) (i < V ? z0[i < V ? i : 0] : z1[i < V ? 0 : i - V]) = i & 1 ? b[i >> 1] : a[i >> 1];
+      p0.pack(z0);
+      p1.pack(z1);
+    }
+  }
+};
+
+// Copies a piece to shared memory behind this thread's back; two bytes are more than cp.async can (they wait here)
+template <int BYTES> __device__ __forceinline__ void copy_piece(unsigned char *to, const void *from) {
+  const uint32_t at = smem_address(to);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(at), "l"(from) : "memory");
+  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+  else *reinterpret_cast<uint16_t *>(to) = *static_cast<const uint16_t *>(from);
 }
 
-// NU units per lane (more than one only where V is small), BACK: the gradients, UB groups of rows in flight per warp
-template <typename T, int V, int NU, bool ADJ, bool BACK, int UB>
-__global__ void __launch_bounds__(kThreads, BACK ? 2 : kBlocksPerSm) qk_rope_kernel(const __grid_constant__ RopeArgs a) {
+__device__ __forceinline__ float group_sum(float x, int group_log2) {
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1)
+    if (o < (1 << group_log2)) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// NU units per lane (more than one only where V is small).  A warp's rows come through a ring in shared memory: every lane
+// copies its own pieces kAhead passes ahead (cp.async, no registers held), and the warp together the table rows of the tokens
+// that these passes begin.
+template <typename T, int V, int NU, bool ADJ, bool BACK>
+__global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_constant__ RopeArgs a) {
+  constexpr int P = BACK ? kBackAhead : kForwardAhead, kPieceBytes = V * (int)sizeof(T), kUnitBytes = 2 * 32 * kPieceBytes;
+  constexpr int kPassBytes = (BACK ? 2 : 1) * NU * kUnitBytes, kTables = P + 1;
+  extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ float sums[BACK ? kWarps : 1][BACK ? STAGE_MAX_HEAD_DIM : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int side = (int)blockIdx.x >= a.side[0].blocks ? 1 : 0;
@@ -84,10 +122,13 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : kBlocksPerSm) qk_rope_ker
   const int block = (int)blockIdx.x - (side ? a.side[0].blocks : 0);
   const int lg = a.group_log2, rows_per_pass = 32 >> lg, row = lane >> lg, unit0 = lane & ((1 << lg) - 1);
   const int half = a.rot >> 1, rest = (a.d - a.rot) >> 1;
+  unsigned char *ring = dyn + warp * (P * kPassBytes + kTables * a.table_bytes);
+  float *tables = reinterpret_cast<float *>(ring + P * kPassBytes);
+  const int table_floats = a.table_bytes / 4;
 
-  int lo_at[NU], hi_at[NU], pair[NU];
+  int at0[NU], at1[NU], pair[NU];   // elements of the unit's pieces, number of its first pair
   bool mine[NU], turned[NU];
-  Chunk<T, V> w_lo[NU], w_hi[NU];
+  float wa[NU][V], wb[NU][V];
   pdl_enter();
 #pragma unroll
   for (int n = 0; n < NU; ++n) {
@@ -95,154 +136,214 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : kBlocksPerSm) qk_rope_ker
     mine[n] = 2 * pair[n] < a.d;
     turned[n] = pair[n] < half;
     if (ADJ) {
-      lo_at[n] = 2 * pair[n];
-      hi_at[n] = lo_at[n] + V;
+      at0[n] = 2 * pair[n];
+      at1[n] = at0[n] + V;
     } else {
-      lo_at[n] = turned[n] ? pair[n] : a.rot + pair[n] - half;
-      hi_at[n] = lo_at[n] + (turned[n] ? half : rest);
+      at0[n] = turned[n] ? pair[n] : a.rot + pair[n] - half;
+      at1[n] = at0[n] + (turned[n] ? half : rest);
     }
     if (mine[n] && s.w != nullptr) {
-      w_lo[n].load(static_cast<const T *>(s.w) + lo_at[n]);
-      w_hi[n].load(static_cast<const T *>(s.w) + hi_at[n]);
+      Unit<T, V, ADJ> w;
+      w.load(static_cast<const T *>(s.w), at0[n], at1[n]);
+      w.get(wa[n], wb[n]);
     } else {
-      float one[V];
 #pragma unroll
-      for (int i = 0; i < V; ++i) one[i] = 1.f;
-      w_lo[n].pack(one);
-      w_hi[n].pack(one);
+      for (int i = 0; i < V; ++i) wa[n][i] = wb[n][i] = 1.f;
     }
   }
-  float dw_lo[NU][V], dw_hi[NU][V];
-  if (BACK) {
+  float dwa[NU][V], dwb[NU][V];
 #pragma unroll
-    for (int n = 0; n < NU; ++n)
+  for (int n = 0; n < NU; ++n)
 #pragma unroll
-      for (int i = 0; i < V; ++i) dw_lo[n][i] = dw_hi[n][i] = 0.f;
-  }
+    for (int i = 0; i < V; ++i) dwa[n][i] = dwb[n][i] = 0.f;
 
-  // this warp's part of the heads, and its tokens
+  // this warp's part of the heads, and its tokens: t0, t0 + slots, ...
   const int wid = block * kWarps + warp, slots = s.blocks * kWarps / s.parts;
   const int part = wid % s.parts;
   const float inv_d = 1.f / (float)a.d;
-  for (int64_t t = wid / s.parts; wid < slots * s.parts && t < a.n; t += slots) {
-    float c[NU][V], sn[NU][V];
-    const int32_t p = a.rot > 0 ? table_row(a, t) : 0;
-#pragma unroll
-    for (int n = 0; n < NU; ++n) {
-      if (mine[n] && turned[n] && p >= 0) {
-        load_floats<V>(a.table + p * a.ldt + pair[n], c[n]);
-        load_floats<V>(a.table + p * a.ldt + half + pair[n], sn[n]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i) c[n][i] = sn[n][i] = 0.f;
+  const int first = part * s.passes * rows_per_pass, heads = min(s.heads - first, s.passes * rows_per_pass);   // of this part
+  const int passes = (heads + rows_per_pass - 1) / rows_per_pass;
+  const int64_t t0 = wid / s.parts;
+  const int64_t steps = wid < slots * s.parts && t0 < a.n ? (a.n - t0 + slots - 1) / slots * passes : 0;   // passes over all its tokens
+  // a pointer goes from pass to pass, and from a token's last pass to the next token's first
+  const T *x = static_cast<const T *>(s.x) + t0 * s.x_token + (first + row) * s.x_head;
+  const T *dy = BACK ? static_cast<const T *>(s.dy) + t0 * s.dy_token + (first + row) * s.dy_head : nullptr;
+  T *out = static_cast<T *>(s.out) + t0 * s.out_token + (first + row) * s.out_head;
+  const int64_t x_step = rows_per_pass * s.x_head, dy_step = rows_per_pass * s.dy_head, out_step = rows_per_pass * s.out_head;
+  const int64_t x_jump = slots * s.x_token - passes * x_step, dy_jump = slots * s.dy_token - passes * dy_step;
+  const int64_t out_jump = slots * s.out_token - passes * out_step;
+
+  // the copies, P passes ahead of the rows in hand
+  int64_t ahead_t = t0, ahead_left = steps;
+  int ahead_row = row, ahead_table = 0;
+  uint32_t ahead_place = 0;
+  int32_t ahead_pos = a.rot > 0 && steps > 0 ? table_row(a, t0) : 0;
+  auto copy_pass = [&]() {
+    if (ahead_left > 0) {
+      --ahead_left;
+      if (ahead_row == row && a.rot > 0) {
+        float *to = tables + ahead_table * table_floats;
+        const float *from = a.table + ahead_pos * a.ldt;
+        if (ahead_pos < 0)
+          for (int i = lane; i < a.rot; i += 32) to[i] = 0.f;
+        else if (a.wide_table)
+          for (int i = lane * 4; i < a.rot; i += 128) copy_piece<16>(reinterpret_cast<unsigned char *>(to + i), from + i);
+        else
+          for (int i = lane; i < a.rot; i += 32) copy_piece<4>(reinterpret_cast<unsigned char *>(to + i), from + i);
+        if (++ahead_table == kTables) ahead_table = 0;
+        ahead_t += slots;
+        if (ahead_t < a.n) ahead_pos = table_row(a, ahead_t);   // known when that token begins
       }
-    }
-    const int first = part * s.passes * rows_per_pass;
-    const int last = min(s.heads, first + s.passes * rows_per_pass);
-    for (int h0 = first + row; h0 - row < last; h0 += UB * rows_per_pass) {
-      Chunk<T, V> x_lo[UB][NU], x_hi[UB][NU], y_lo[BACK ? UB : 1][NU], y_hi[BACK ? UB : 1][NU];
-#pragma unroll
-      for (int b = 0; b < UB; ++b) {
-        const int h = h0 + b * rows_per_pass;
-        const T *x = static_cast<const T *>(s.x) + t * s.x_token + h * s.x_head;
-        const T *dy = BACK ? static_cast<const T *>(s.dy) + t * s.dy_token + h * s.dy_head : nullptr;
-#pragma unroll
-        for (int n = 0; n < NU; ++n) {
-          float zero[V];
-#pragma unroll
-          for (int i = 0; i < V; ++i) zero[i] = 0.f;
-          if (mine[n] && h < last) {
-            x_lo[b][n].load(x + lo_at[n]);
-            x_hi[b][n].load(x + hi_at[n]);
-            if (BACK) {
-              y_lo[b][n].load(dy + lo_at[n]);
-              y_hi[b][n].load(dy + hi_at[n]);
-            }
-          } else {
-            x_lo[b][n].pack(zero);
-            x_hi[b][n].pack(zero);
-            if (BACK) {
-              y_lo[b][n].pack(zero);
-              y_hi[b][n].pack(zero);
-            }
-          }
-        }
-      }
-#pragma unroll
-      for (int b = 0; b < UB; ++b) {
-        const int h = h0 + b * rows_per_pass;
-        float sq = 0.f;
+      if (ahead_row < heads) {
+        unsigned char *to = ring + ahead_place + lane * kPieceBytes;
 #pragma unroll
         for (int n = 0; n < NU; ++n)
-#pragma unroll
-          for (int i = 0; i < V; ++i) {
-            sq = fmaf(x_lo[b][n].get(i), x_lo[b][n].get(i), sq);
-            sq = fmaf(x_hi[b][n].get(i), x_hi[b][n].get(i), sq);
-          }
-        for (int o = (1 << lg) >> 1; o > 0; o >>= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        const float r = __frsqrt_rn(fmaf(sq, inv_d, a.eps));
-        T *out = static_cast<T *>(s.out) + t * s.out_token + h * s.out_head;
-        if (!BACK) {
-#pragma unroll
-          for (int n = 0; n < NU; ++n) {
-            float lo[V], hi[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              lo[i] = x_lo[b][n].get(i) * r * w_lo[n].get(i);
-              hi[i] = x_hi[b][n].get(i) * r * w_hi[n].get(i);
-            }
-            if (turned[n]) turn<V, ADJ>(lo, hi, c[n], sn[n], 1.f);
-            if (mine[n] && h < last) {
-              Chunk<T, V> o;
-              o.pack(lo);
-              o.store(out + lo_at[n]);
-              o.pack(hi);
-              o.store(out + hi_at[n]);
+          if (mine[n]) {
+            copy_piece<kPieceBytes>(to + n * kUnitBytes, x + at0[n]);
+            copy_piece<kPieceBytes>(to + n * kUnitBytes + 32 * kPieceBytes, x + at1[n]);
+            if (BACK) {
+              copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes, dy + at0[n]);
+              copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes + 32 * kPieceBytes, dy + at1[n]);
             }
           }
-        } else {
-          float g_lo[NU][V], g_hi[NU][V], inner = 0.f;
+      }
+      ahead_row += rows_per_pass;
+      x += x_step;
+      if (BACK) dy += dy_step;
+      if (ahead_row - row >= heads) {
+        ahead_row = row;
+        x += x_jump;
+        if (BACK) dy += dy_jump;
+      }
+      ahead_place += kPassBytes;
+      if (ahead_place == P * kPassBytes) ahead_place = 0;
+    }
+    asm volatile("cp.async.commit_group;\n" ::: "memory");
+  };
+#pragma unroll 1
+  for (int i = 0; i < P; ++i) copy_pass();
+
+  // forward: y_a = r (x_a (w_a cos) - x_b (w_b sin)), y_b = r (x_b (w_b cos) + x_a (w_a sin)); the products of the gain and the
+  // angle serve all heads of the token.  backward: cosine, sine, minus sine.
+  float ca[NU][V], cb[BACK ? 1 : NU][V], sa[NU][V], sb[NU][V];
+  int now = row, table = 0;   // the lane's row among the part's heads
+  uint32_t place_at = 0;
+#pragma unroll 1
+  for (int64_t left = steps; left > 0; --left) {
+    asm volatile("cp.async.wait_group %0;\n" ::"n"(P - 1) : "memory");
+    __syncwarp();
+    if (now == row) {   // a token's first pass
+      const float *cs = tables + table * table_floats;
 #pragma unroll
-          for (int n = 0; n < NU; ++n) {
+      for (int n = 0; n < NU; ++n)
+        if (mine[n] && turned[n]) {
+          float c[V], sn[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-              g_lo[n][i] = y_lo[b][n].get(i);
-              g_hi[n][i] = y_hi[b][n].get(i);
-            }
-            if (turned[n]) turn<V, ADJ>(g_lo[n], g_hi[n], c[n], sn[n], -1.f);
+          for (int i = 0; i < V; ++i) c[i] = cs[pair[n] + i], sn[i] = cs[half + pair[n] + i];
+          if (BACK) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-              const float u_lo = x_lo[b][n].get(i) * r, u_hi = x_hi[b][n].get(i) * r;
-              // a row past the last head, or a column past D, is made of zeros: it adds nothing
-              dw_lo[n][i] = fmaf(g_lo[n][i], u_lo, dw_lo[n][i]);
-              dw_hi[n][i] = fmaf(g_hi[n][i], u_hi, dw_hi[n][i]);
-              g_lo[n][i] *= w_lo[n].get(i);
-              g_hi[n][i] *= w_hi[n].get(i);
-              inner = fmaf(g_lo[n][i], u_lo, inner);
-              inner = fmaf(g_hi[n][i], u_hi, inner);
-            }
-          }
-          for (int o = (1 << lg) >> 1; o > 0; o >>= 1) inner += __shfl_xor_sync(0xffffffffu, inner, o);
-          inner *= inv_d;
-#pragma unroll
-          for (int n = 0; n < NU; ++n) {
-            float lo[V], hi[V];
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-              lo[i] = r * fmaf(-(x_lo[b][n].get(i) * r), inner, g_lo[n][i]);
-              hi[i] = r * fmaf(-(x_hi[b][n].get(i) * r), inner, g_hi[n][i]);
-            }
-            if (mine[n] && h < last) {
-              Chunk<T, V> o;
-              o.pack(lo);
-              o.store(out + lo_at[n]);
-              o.pack(hi);
-              o.store(out + hi_at[n]);
-            }
+            for (int i = 0; i < V; ++i) ca[n][i] = c[i], sa[n][i] = sn[i], sb[n][i] = -sn[i];
+          } else {
+            v_mul(ca[n], wa[n], c);
+            v_mul(cb[BACK ? 0 : n], wb[n], c);
+            v_mul(sa[n], wa[n], sn);
+            v_mul(sb[n], wb[n], sn);
+            v_scale(sb[n], -1.f, sb[n]);
           }
         }
+      if (++table == kTables) table = 0;
+    }
+    const bool there = now < heads;
+    const unsigned char *place = ring + place_at + lane * kPieceBytes;
+    float xa[NU][V], xb[NU][V], oa[NU][V], ob[NU][V], sq[V] = {};
+#pragma unroll
+    for (int n = 0; n < NU; ++n) {
+      Unit<T, V, ADJ> u;
+      if (mine[n] && there) {
+        u.take(place + n * kUnitBytes);
+      } else {   // zeros: they add nothing to a sum
+        const float zero[V] = {};
+        u.pack(zero, zero);
+      }
+      u.get(xa[n], xb[n]);
+      v_fma(sq, xa[n], xa[n], sq);
+      v_fma(sq, xb[n], xb[n], sq);
+    }
+    const float r = rsqrtf(fmaf(group_sum(v_total(sq), lg), inv_d, a.eps));
+    if (!BACK) {
+#pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        v_scale(xa[n], r, xa[n]);
+        v_scale(xb[n], r, xb[n]);
+        if (turned[n]) {
+          v_mul(oa[n], xa[n], ca[n]);
+          v_fma(oa[n], xb[n], sb[n], oa[n]);
+          v_mul(ob[n], xb[n], cb[BACK ? 0 : n]);
+          v_fma(ob[n], xa[n], sa[n], ob[n]);
+        } else {
+          v_mul(oa[n], xa[n], wa[n]);
+          v_mul(ob[n], xb[n], wb[n]);
+        }
+      }
+    } else {
+      // g: the gradient turned back; sums of g x w for the row and of g x r for the gain
+      float in[V] = {};
+#pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        Unit<T, V, ADJ> u;
+        if (mine[n] && there) {
+          u.take(place + (NU + n) * kUnitBytes);
+        } else {
+          const float zero[V] = {};
+          u.pack(zero, zero);
+        }
+        float ga[V], gb[V];
+        u.get(ga, gb);
+        if (turned[n]) {
+          float ta[V];
+          v_mul(ta, ga, ca[n]);
+          v_fma(ta, gb, sa[n], ta);
+          v_mul(gb, gb, ca[n]);
+          v_fma(gb, ga, sb[n], gb);
+#pragma unroll
+          for (int i = 0; i < V; ++i) ga[i] = ta[i];
+        }
+        float q[V];
+        v_mul(q, ga, xa[n]);
+        v_axpy(dwa[n], r, q, dwa[n]);
+        v_fma(in, q, wa[n], in);
+        v_mul(q, gb, xb[n]);
+        v_axpy(dwb[n], r, q, dwb[n]);
+        v_fma(in, q, wb[n], in);
+        v_mul(ga, ga, wa[n]);
+        v_mul(gb, gb, wb[n]);
+        v_scale(oa[n], r, ga);
+        v_scale(ob[n], r, gb);
+      }
+      const float k = -(r * (r * (r * (group_sum(v_total(in), lg) * inv_d))));   // dx = r (g w - x r^2 mean(g w x))
+#pragma unroll
+      for (int n = 0; n < NU; ++n) {
+        v_axpy(oa[n], k, xa[n], oa[n]);
+        v_axpy(ob[n], k, xb[n], ob[n]);
       }
     }
+#pragma unroll
+    for (int n = 0; n < NU; ++n)
+      if (mine[n] && there) {
+        Unit<T, V, ADJ> o;
+        o.pack(oa[n], ob[n]);
+        o.store(out, at0[n], at1[n]);
+      }
+    out += out_step;
+    now += rows_per_pass;
+    if (now - row >= heads) {
+      now = row;
+      out += out_jump;
+    }
+    place_at += kPassBytes;
+    if (place_at == P * kPassBytes) place_at = 0;
+    __syncwarp();
+    copy_pass();
   }
 
   if (BACK && s.partial != nullptr) {   // the block's share of dw: lanes of one column, then warps, always in the same order
@@ -251,12 +352,12 @@ __global__ void __launch_bounds__(kThreads, BACK ? 2 : kBlocksPerSm) qk_rope_ker
 #pragma unroll
       for (int i = 0; i < V; ++i) {
         for (int o = 16; o >= (1 << lg); o >>= 1) {
-          dw_lo[n][i] += __shfl_xor_sync(0xffffffffu, dw_lo[n][i], o);
-          dw_hi[n][i] += __shfl_xor_sync(0xffffffffu, dw_hi[n][i], o);
+          dwa[n][i] += __shfl_xor_sync(0xffffffffu, dwa[n][i], o);
+          dwb[n][i] += __shfl_xor_sync(0xffffffffu, dwb[n][i], o);
         }
         if (row == 0 && mine[n]) {
-          sums[warp][lo_at[n] + i] = dw_lo[n][i];
-          sums[warp][hi_at[n] + i] = dw_hi[n][i];
+          sums[warp][at0[n] + (ADJ ? 2 * i : i)] = dwa[n][i];
+          sums[warp][ADJ ? at0[n] + 2 * i + 1 : at1[n] + i] = dwb[n][i];
         }
       }
     __syncthreads();
@@ -344,9 +445,6 @@ struct Width {
   void stride(int64_t s) {
     while (v > 1 && s % v != 0) v >>= 1;
   }
-  void table(const void *p, int64_t ld) {
-    while (v > 1 && (reinterpret_cast<uintptr_t>(p) % (4 * (v < 4 ? v : 4)) != 0 || ld % (v < 4 ? v : 4) != 0)) v >>= 1;
-  }
 };
 
 void plan_side(RopeSide &s, int64_t n, int rows_per_pass, int max_blocks) {
@@ -364,22 +462,33 @@ void plan_side(RopeSide &s, int64_t n, int rows_per_pass, int max_blocks) {
   if (s.blocks < least) s.blocks = (int32_t)least;   // a slot for every part
 }
 
-// The most blocks a side gets: the resident ones, dealt by heads
-int side_blocks(int sms, int per_sm, int32_t heads, int32_t other) {
+// The most blocks a side gets: the resident ones, dealt by a token's passes; its table row costs about one more
+int side_blocks(int sms, int per_sm, int32_t heads, int32_t other, int rows_per_pass) {
   if (heads == 0) return 0;
-  const int64_t b = (int64_t)sms * per_sm * heads / ((int64_t)heads + other);
+  auto cost = [&](int32_t h) { return h == 0 ? 0 : (int64_t)(h + rows_per_pass - 1) / rows_per_pass + 1; };
+  const int64_t b = (int64_t)sms * per_sm * cost(heads) / (cost(heads) + cost(other));
   return b < 1 ? 1 : (int)b;
+}
+
+template <typename T, int V, int NU, bool ADJ, bool BACK>
+cudaError_t launch_unit(const RopeArgs &a, cudaStream_t stream) {
+  static std::atomic<uint64_t> allowed{0};
+  constexpr int P = BACK ? kBackAhead : kForwardAhead;
+  constexpr int kRing = kWarps * P * (BACK ? 2 : 1) * NU * 2 * 32 * V * (int)sizeof(T);
+  auto kernel = qk_rope_kernel<T, V, NU, ADJ, BACK>;
+  const cudaError_t e = allow_dynamic_smem(kernel, kRing + kWarps * (P + 1) * STAGE_MAX_HEAD_DIM * 4, allowed);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(kernel, (unsigned)(a.side[0].blocks + a.side[1].blocks), kThreads, kRing + kWarps * (P + 1) * a.table_bytes, stream, 1, a);
 }
 
 template <typename T, bool ADJ, bool BACK>
 cudaError_t launch_width(const RopeArgs &a, int v, cudaStream_t stream) {
-  const unsigned grid = (unsigned)(a.side[0].blocks + a.side[1].blocks);
   if constexpr (sizeof(T) == 2) {
-    if (v == 8) return launch_dependent(qk_rope_kernel<T, 8, 1, ADJ, BACK, 2>, grid, kThreads, 0, stream, 1, a);
+    if (v == 8) return launch_unit<T, 8, 1, ADJ, BACK>(a, stream);
   }
-  if (v >= 4) return launch_dependent(qk_rope_kernel<T, 4, 1, ADJ, BACK, 2>, grid, kThreads, 0, stream, 1, a);
-  if (v == 2) return launch_dependent(qk_rope_kernel<T, 2, 2, ADJ, BACK, 1>, grid, kThreads, 0, stream, 1, a);
-  return launch_dependent(qk_rope_kernel<T, 1, 4, ADJ, BACK, 1>, grid, kThreads, 0, stream, 1, a);
+  if (v >= 4) return launch_unit<T, 4, 1, ADJ, BACK>(a, stream);
+  if (v == 2) return launch_unit<T, 2, 2, ADJ, BACK>(a, stream);
+  return launch_unit<T, 1, 4, ADJ, BACK>(a, stream);
 }
 
 template <bool BACK>
@@ -394,12 +503,12 @@ ssn_status_t launch_rope(const stage_qk_rope_t *op, RopeArgs &a, int v, cudaStre
 }
 
 // Lanes per row and the blocks of both sides
-void plan(const stage_qk_rope_t *op, RopeArgs &a, int v, int per_sm) {
+void plan(const stage_qk_rope_t *op, RopeArgs &a, int v) {
   const int units = (op->head_dim / 2 + v - 1) / v;
   a.group_log2 = 0;
   while ((1 << a.group_log2) < units && a.group_log2 < 5) ++a.group_log2;
   const int sms = stage_sm_count(), rows = 32 >> a.group_log2;
-  for (int i = 0; i < 2; ++i) plan_side(a.side[i], a.n, rows, side_blocks(sms, per_sm, a.side[i].heads, a.side[1 - i].heads));
+  for (int i = 0; i < 2; ++i) plan_side(a.side[i], a.n, rows, side_blocks(sms, kPerSm, a.side[i].heads, a.side[1 - i].heads, rows));
 }
 
 void fill(const stage_qk_rope_t *op, RopeArgs &a, const int32_t *pos, int64_t n, int32_t seq_len) {
@@ -413,6 +522,8 @@ void fill(const stage_qk_rope_t *op, RopeArgs &a, const int32_t *pos, int64_t n,
   a.max_pos = op->max_pos;
   a.seq_len = seq_len;
   a.eps = op->eps;
+  a.table_bytes = (op->rot_dim * 4 + 15) / 16 * 16;
+  a.wide_table = op->rot_dim > 0 && op->rot_dim % 4 == 0 && op->ldt % 4 == 0 && aligned_to(op->table, 16);
   a.side[0].w = op->wq;
   a.side[1].w = op->wk;
 }
@@ -422,7 +533,6 @@ int width_of(const stage_qk_rope_t *op, const RopeArgs &a, bool back) {
   Width w(item);
   w.stride(a.rot / 2);
   w.stride((a.d - a.rot) / 2);
-  if (a.rot > 0) w.table(a.table, a.ldt);
   for (const RopeSide &s : a.side) {
     if (s.heads == 0) continue;
     w.address(s.x, item);
@@ -437,8 +547,6 @@ int width_of(const stage_qk_rope_t *op, const RopeArgs &a, bool back) {
   }
   return w.v;
 }
-
-constexpr int kBackPerSm = 2;   // resident blocks of the backward kernel (its launch bounds)
 
 }  // namespace
 }  // namespace ssn
@@ -478,14 +586,14 @@ ssn_status_t stage_qk_rope_forward(const stage_qk_rope_t *op, const void *q, int
   a.side[0] = qs;
   a.side[1] = ks;
   const int v = width_of(op, a, false);
-  plan(op, a, v, kBlocksPerSm);
+  plan(op, a, v);
   return launch_rope<false>(op, a, v, static_cast<cudaStream_t>(stream));
 }
 
 // Partial sums of at most the resident blocks, D floats each (a side never has fewer than a slot per part of its heads)
 size_t stage_qk_rope_workspace_bytes(const stage_qk_rope_t *op, int64_t n_tokens, int32_t q_heads, int32_t k_heads) {
   if (check_op(op) != SSN_OK || n_tokens <= 0 || q_heads < 0 || k_heads < 0) return 0;
-  const int64_t resident = (int64_t)stage_sm_count() * kBackPerSm + 2;
+  const int64_t resident = (int64_t)stage_sm_count() * kPerSm + 2;
   return (size_t)(resident + ((int64_t)q_heads + k_heads) / kWarps + 2) * op->head_dim * sizeof(float);
 }
 
@@ -521,7 +629,7 @@ ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, i
     a.side[0] = qs;
     a.side[1] = ks;
     const int v = width_of(op, a, true);
-    plan(op, a, v, kBackPerSm);
+    plan(op, a, v);
     float *partial = static_cast<float *>(workspace);
     if (dwq != nullptr) a.side[0].partial = partial;
     if (dwk != nullptr) a.side[1].partial = partial + (int64_t)a.side[0].blocks * d;
