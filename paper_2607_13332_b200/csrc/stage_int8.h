@@ -14,7 +14,44 @@ struct Int8Matmul {
   int32_t *dev_status;
 };
 
-// tcgen05 kernels: operand rows on 16-byte boundaries.  cudaErrorNotSupported, with nothing launched, for others.
-cudaError_t launch_int8_umma(const Int8Matmul &a, bool f32, int sm_count, cudaStream_t stream);
+// tcgen05 kernels.  rows16: all operand rows start on 16-byte boundaries.
+cudaError_t launch_int8_umma(const Int8Matmul &a, bool f32, bool rows16, int sm_count, cudaStream_t stream);
+
+#ifdef __CUDACC__
+// The first `bytes` (1 .. 16) bytes of v, zeros behind them
+__device__ __forceinline__ uint4 first_bytes(uint4 v, int bytes) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int keep = min(max(bytes - 4 * i, 0), 4);
+    w[i] = keep == 0 ? 0u : w[i] & (0xffffffffu >> (32 - 8 * keep));
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Bytes [at, at + 16) of a row of `bytes` bytes that starts anywhere, zeros past its end: the one or two aligned 16-byte pieces
+// that hold some of them (a piece with a byte of the row in it is memory of the row's buffer), shifted together.
+__device__ __forceinline__ uint4 load_row16(const int8_t *row, int at, int bytes) {
+  if (at >= bytes) return make_uint4(0, 0, 0, 0);
+  const uintptr_t p = reinterpret_cast<uintptr_t>(row + at);
+  const int off = (int)(p & 15), there = min(bytes - at, 16);
+  const uint4 *from = reinterpret_cast<const uint4 *>(p - off);
+  uint4 lo = __ldg(from), hi = make_uint4(0, 0, 0, 0);
+  if (off + there > 16) hi = __ldg(from + 1);
+  const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+  // by whole words first, then by bytes
+  uint32_t a[5];
+  const int words = off >> 2;
+#pragma unroll
+  for (int i = 0; i < 5; ++i) {
+    const uint32_t s01 = words & 1 ? (i + 1 < 8 ? w[i + 1] : 0u) : w[i], s23 = words & 1 ? (i + 3 < 8 ? w[i + 3] : 0u) : (i + 2 < 8 ? w[i + 2] : 0u);
+    a[i] = words & 2 ? s23 : s01;
+  }
+  const uint32_t by = 8 * (off & 3);
+  const uint4 v = make_uint4(__funnelshift_r(a[0], a[1], by), __funnelshift_r(a[1], a[2], by), __funnelshift_r(a[2], a[3], by),
+                             __funnelshift_r(a[3], a[4], by));
+  return there < 16 ? first_bytes(v, there) : v;
+}
+#endif
 
 }  // namespace ssn

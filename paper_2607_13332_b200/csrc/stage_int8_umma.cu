@@ -6,17 +6,21 @@
 namespace ssn {
 namespace {
 
-template <int CG, int BN, bool SWAP, typename T>
+template <int CG, int BN, bool SWAP, typename T, bool RAGGED = false>
 cudaError_t launch_tiles(const Int8Matmul &m, int split, int sm_count, cudaStream_t stream) {
-  using Cfg = Int8Config<CG, BN, SWAP>;
+  using Cfg = Int8Config<CG, BN, SWAP, RAGGED>;
   static std::atomic<uint64_t> allowed{0};
-  auto kernel = int8_umma_kernel<CG, BN, SWAP, T>;
-  Int8Maps maps;
-  const int8_t *pa = SWAP ? m.wq : m.xq, *pb = SWAP ? m.xq : m.wq;
-  const int64_t ra = SWAP ? m.outer : m.n, rb = SWAP ? m.n : m.outer, la = SWAP ? m.ldw : m.ldx, lb = SWAP ? m.ldx : m.ldw;
-  if (!make_sw128_map_u8(&maps.a, pa, ra, m.inner, la, 128) || !make_sw128_map_u8(&maps.b, pb, rb, m.inner, lb, Cfg::kBRows))
-    return cudaErrorNotSupported;
+  auto kernel = int8_umma_kernel<CG, BN, SWAP, RAGGED, T>;
+  Int8Maps maps{};
   Int8Args a{};
+  a.a = SWAP ? m.wq : m.xq;
+  a.b = SWAP ? m.xq : m.wq;
+  const int64_t ra = SWAP ? m.outer : m.n, rb = SWAP ? m.n : m.outer;
+  a.lda = SWAP ? m.ldw : m.ldx;
+  a.ldb = SWAP ? m.ldx : m.ldw;
+  a.inner = (int32_t)m.inner;
+  if (!RAGGED && (!make_sw128_map_u8(&maps.a, a.a, ra, m.inner, a.lda, 128) || !make_sw128_map_u8(&maps.b, a.b, rb, m.inner, a.ldb, Cfg::kBRows)))
+    return cudaErrorNotSupported;
   a.sa = SWAP ? m.ws : m.xs;
   a.sb = SWAP ? m.xs : m.ws;
   a.y = m.y;
@@ -33,40 +37,53 @@ cudaError_t launch_tiles(const Int8Matmul &m, int split, int sm_count, cudaStrea
   const int64_t tiles = (int64_t)a.tiles_a * a.tiles_b;
   int64_t workers = split > 1 ? tiles : sm_count / CG;   // a splitting cluster has one tile
   if (workers > tiles) workers = tiles;
-  return launch_dependent(kernel, (unsigned)(workers * cluster), kInt8Threads, Cfg::kSmemBytes, stream, cluster, a, maps);
+  return launch_dependent(kernel, (unsigned)(workers * cluster), Cfg::kThreads, Cfg::kSmemBytes, stream, cluster, a, maps);
+}
+
+// CTAs per tile of 128 channels, while there are SMs for them and each keeps a few steps of the inner dimension
+int split_of(const Int8Matmul &m, int sms) {
+  const int64_t steps = (m.inner + kInt8Step - 1) / kInt8Step, tiles = (m.outer + 127) / 128;
+  int split = 1;
+  while (split < 8 && tiles * split * 2 <= sms && steps >= split * 4) split *= 2;
+  return split;
+}
+
+template <typename T> cudaError_t launch_ragged(const Int8Matmul &m, int sms, cudaStream_t stream) {
+  if (m.n <= 16) return launch_tiles<1, 16, true, T, true>(m, split_of(m, sms), sms, stream);
+  if (m.n <= 64) return launch_tiles<1, 64, true, T, true>(m, split_of(m, sms), sms, stream);
+  return launch_tiles<1, 128, false, T, true>(m, 1, sms, stream);
 }
 
 template <typename T> cudaError_t launch_typed(const Int8Matmul &m, int sms, cudaStream_t stream) {
-  const int64_t steps = (m.inner + kInt8Step - 1) / kInt8Step;
-  if (m.n <= 256) {   // few tokens: weights on the M side
-    const int64_t tiles = (m.outer + 127) / 128;
-    int split = 1;   // CTAs per tile, while there are SMs for them and each keeps a few steps
-    while (m.n <= 64 && split < 8 && tiles * split * 2 <= sms && steps >= split * 4) split *= 2;
-    if (m.n <= 16) return launch_tiles<1, 16, true, T>(m, split, sms, stream);
-    if (m.n <= 32) return launch_tiles<1, 32, true, T>(m, split, sms, stream);
-    if (m.n <= 64) return launch_tiles<1, 64, true, T>(m, split, sms, stream);
-    if (m.n <= 128) return launch_tiles<1, 128, true, T>(m, 1, sms, stream);
-    return launch_tiles<1, 256, true, T>(m, 1, sms, stream);
-  }
-  // The tile width whose last wave leaves the fewest SMs idle, a narrower tile counted as slower per column.
-  const int64_t pairs = sms / 2 > 0 ? sms / 2 : 1, ta = (m.n + 255) / 256;
-  auto cost = [&](int64_t bn, int64_t per_tile) { return (ta * ((m.outer + bn - 1) / bn) + pairs - 1) / pairs * per_tile; };
-  if (cost(128, 150) < cost(256, 256)) return launch_tiles<2, 128, false, T>(m, 1, sms, stream);
+  if (m.n <= 16) return launch_tiles<1, 16, true, T>(m, split_of(m, sms), sms, stream);
+  if (m.n <= 32) return launch_tiles<1, 32, true, T>(m, split_of(m, sms), sms, stream);
+  if (m.n <= 64) return launch_tiles<1, 64, true, T>(m, split_of(m, sms), sms, stream);
+  // The shape whose waves of tiles take the least time: a step of a wave of pairs of 256 x 256 takes about 0.38 us, of CTAs of
+  // 128 x 256 0.42 (each loads B for itself), of the narrower ones 0.26; a wave's first loads and a tile's output cost as much as
+  // some 8 and 5 steps.  Measured (us; pairs 256, pairs 128, CTAs 256, CTAs 128): 777 x 2000 x 5003 22.8 / 22.9 / 18.0 / 20.2,
+  // 128 x 4096 x 4096 15.3 / 14.0 / 14.8 / 13.4, 256 x 4096 x 128256 113 / 144 / 125 / 149, 16384 x 256 x 4096 60 / 75 / 53 / 60.
+  const double steps = (double)((m.inner + kInt8Step - 1) / kInt8Step);
+  auto time = [&](int64_t ta, int64_t bn, int64_t workers, double step, double rest) {
+    const int64_t tiles = ta * ((m.outer + bn - 1) / bn), waves = (tiles + workers - 1) / workers;
+    return (double)waves * (step * steps > rest ? step * steps : rest) + rest;
+  };
+  const int64_t half = (m.n + 127) / 128, whole = (m.n + 255) / 256;
+  const double pairs = time(whole, 256, sms / 2, 0.38, 4.0), wide = time(half, 256, sms, 0.42, 3.5), narrow = time(half, 128, sms, 0.28, 3.0);
+  if (wide < pairs && wide <= narrow) return launch_tiles<1, 256, false, T>(m, 1, sms, stream);
+  if (narrow < pairs) return launch_tiles<1, 128, false, T>(m, 1, sms, stream);
   return launch_tiles<2, 256, false, T>(m, 1, sms, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_int8_umma(const Int8Matmul &given, bool f32, int sm_count, cudaStream_t stream) {
-  Int8Matmul m = given;   // the pitch of a single row does not matter
-  if (m.n == 1) m.ldx = (m.inner + 15) / 16 * 16;
-  if (m.outer == 1) m.ldw = (m.inner + 15) / 16 * 16;
-  if (((reinterpret_cast<uintptr_t>(m.xq) | reinterpret_cast<uintptr_t>(m.wq) | (uintptr_t)m.ldx | (uintptr_t)m.ldw) & 15) != 0)
-    return cudaErrorNotSupported;
-  // row coordinates and strides a tensor map can hold
-  constexpr int64_t kRows = 0x7fffff00, kPitch = (int64_t)1 << 40;
-  if (m.n > kRows || m.outer > kRows || m.ldx >= kPitch || m.ldw >= kPitch || sm_count < 2) return cudaErrorNotSupported;
-  return f32 ? launch_typed<float>(m, sm_count, stream) : launch_typed<__nv_bfloat16>(m, sm_count, stream);
+cudaError_t launch_int8_umma(const Int8Matmul &m, bool f32, bool rows16, int sm_count, cudaStream_t stream) {
+  if (sm_count < 2) sm_count = 2;
+  constexpr int64_t kPitch = (int64_t)1 << 40;   // of a tensor map
+  if (rows16 && m.ldx < kPitch && m.ldw < kPitch) {
+    const cudaError_t e = f32 ? launch_typed<float>(m, sm_count, stream) : launch_typed<__nv_bfloat16>(m, sm_count, stream);
+    if (e != cudaErrorNotSupported) return e;
+  }
+  return f32 ? launch_ragged<float>(m, sm_count, stream) : launch_ragged<__nv_bfloat16>(m, sm_count, stream);
 }
 
 }  // namespace ssn

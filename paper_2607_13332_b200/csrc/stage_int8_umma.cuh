@@ -7,11 +7,14 @@
 //                   tiles than SMs a cluster splits the inner dimension and adds its partial sums through distributed shared
 //                   memory (integers: any order gives the same sum).
 //
+//   CG = 1, !SWAP   A = tokens, B = channels, a CTA by itself: sizes whose tiles of pairs would leave many SMs out.
+//
 //   warp 0     producer: per stage of 128 bytes of the inner dimension one TMA box of A and one of B, 128-byte swizzled; the
 //              inner dimension's tail and rows past the end are filled with zeros, which add nothing
 //   warp 1     MMA issuer (of the pair's first CTA), four K steps of 32 bytes per stage
 //   warps 4-7  epilogue: tcgen05.ld of the 32 lanes each may read, scaling, stores; two accumulators, so that a tile's
 //              epilogue runs behind the next tile's MMAs
+//   8 more     (RAGGED: rows off 16-byte boundaries, which TMA cannot fetch) load and shift them into the stages instead
 #pragma once
 
 #include <cuda.h>
@@ -31,15 +34,20 @@ struct Int8Args {
   void *y;
   int64_t ldy;
   int32_t rows_a, rows_b, steps, tiles_a, tiles_b;   // steps of kInt8Step bytes
+  const int8_t *a, *b;                               // the operands, for loads that TMA cannot do
+  int64_t lda, ldb;
+  int32_t inner;
   int32_t *dev_status;
 };
 
-constexpr int kInt8Step = 128, kInt8Threads = 256;
+constexpr int kInt8Step = 128, kInt8Loaders = 256;
 
-template <int CG, int BN, bool SWAP> struct Int8Config {
+template <int CG, int BN, bool SWAP, bool RAGGED> struct Int8Config {
+  static_assert(CG == 1 || !RAGGED, "pairs of CTAs fetch by TMA");
+  static constexpr int kFirstLoader = 256, kThreads = kFirstLoader + (RAGGED ? kInt8Loaders : 0);
   static constexpr int kABytes = 128 * kInt8Step, kBRows = BN / CG, kBBytes = kBRows * kInt8Step;
   static constexpr int kStageBytes = kABytes + kBBytes;
-  static constexpr int kOutBytes = SWAP ? 0 : 4 * 4096;   // a 32 x 128-byte block of the output per epilogue warp
+  static constexpr int kOutBytes = SWAP ? 0 : 4 * (4096 + BN * 4);   // per epilogue warp a 32 x 128-byte block of the output, and B's scales
   static constexpr int kBudget = 222 * 1024 - kOutBytes;
   static constexpr int kFit = kBudget / kStageBytes, kStages = kFit < 10 ? kFit : 10;
   static constexpr int kBars = 2 * kStages + 5;
@@ -76,9 +84,10 @@ template <int CG> __device__ __forceinline__ void int8_commit(uint32_t bar) {
   else
     umma_commit(bar);
 }
-template <int CG, int BN, bool SWAP, typename T>
-__global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
-  using Cfg = Int8Config<CG, BN, SWAP>;
+template <int CG, int BN, bool SWAP, bool RAGGED, typename T>
+__global__ void __launch_bounds__((Int8Config<CG, BN, SWAP, RAGGED>::kThreads), 1)
+int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
+  using Cfg = Int8Config<CG, BN, SWAP, RAGGED>;
   constexpr int S = Cfg::kStages;
   extern __shared__ __align__(128) unsigned char smem_raw[];
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
@@ -97,7 +106,7 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Ar
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < S; ++s) {
-      mbar_init(full_bar(s), 1);
+      mbar_init(full_bar(s), RAGGED ? kInt8Loaders / 32 : 1);
       mbar_init(empty_bar(s), 1);
     }
     for (int b = 0; b < 2; ++b) {
@@ -145,10 +154,58 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Ar
   };
 
   uint32_t v[BN <= 64 ? BN : 1];   // a splitting CTA's partial sums
-  if (warp == 0) {
+  if (RAGGED && threadIdx.x >= Cfg::kFirstLoader) {
+    // Loader warps: 16 bytes per lane and piece, eight lanes to a row's 128 bytes, into the layout that TMA would write
+    const int loader = threadIdx.x - Cfg::kFirstLoader, piece = loader & 7, row0 = loader >> 3;
+    constexpr int kRowStep = kInt8Loaders / 8, kRows = 128 + Cfg::kBRows, kPerThread = (kRows + kRowStep - 1) / kRowStep;
+    int slot = 0;
+    uint32_t parity = 1;
+    for (int64_t tile = worker; tile < tiles && !dead; tile += workers) {
+      int ta, tb;
+      place(tile, ta, tb);
+      uint4 v[kPerThread], next[kPerThread];
+      auto fetch = [&](uint4 (&to)[kPerThread], int st) {
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+          const int r = row0 + i * kRowStep;
+          const bool is_a = r < 128;
+          const int64_t row = is_a ? (int64_t)ta * 128 + r : (int64_t)tb * BN + r - 128;
+          to[i] = make_uint4(0, 0, 0, 0);
+          if (r < kRows && row < (is_a ? a.rows_a : a.rows_b))
+            to[i] = load_row16(is_a ? a.a + row * a.lda : a.b + row * a.ldb, st * kInt8Step + piece * 16, a.inner);
+        }
+      };
+      fetch(next, step_lo);
+      for (int st = step_lo; st < step_hi; ++st) {
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) v[i] = next[i];
+        if (st + 1 < step_hi) fetch(next, st + 1);   // on its way while this one is stored
+        if (!dead && !mbar_wait(empty_bar(slot), parity)) {
+          timed_out();
+          break;
+        }
+        const uint32_t base = smem0 + (uint32_t)slot * Cfg::kStageBytes;
+#pragma unroll
+        for (int i = 0; i < kPerThread; ++i) {
+          const int r = row0 + i * kRowStep;   // B's rows follow A's: both start on swizzle blocks
+          if (r < kRows)
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};\n" ::"r"(base + r * 128 + ((piece ^ (r & 7)) << 4)), "r"(v[i].x), "r"(v[i].y),
+                         "r"(v[i].z), "r"(v[i].w) : "memory");
+        }
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(full_bar(slot));
+        if (++slot == S) {
+          slot = 0;
+          parity ^= 1u;
+        }
+      }
+    }
+    __syncwarp();
+  } else if (warp == 0) {
     int slot = 0, issued = 0;
     uint32_t parity = 1;
-    if (lane == 0) {
+    if (!RAGGED && lane == 0) {
       for (int64_t tile = worker; tile < tiles && !dead; tile += workers) {
         int ta, tb;
         place(tile, ta, tb);
@@ -215,22 +272,36 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Ar
       }
     }
     __syncwarp();
-  } else if (warp >= 4) {
+  } else if (warp >= 4 && threadIdx.x < Cfg::kFirstLoader) {
     const int quarter = warp & 3;
+    const uint32_t scales = out0 + 4 * 4096 + (uint32_t)quarter * BN * 4;   // !SWAP
     int count = 0;
     for (int64_t tile = worker; tile < tiles && !dead; tile += workers, ++count) {
       int ta, tb;
       place(tile, ta, tb);
       const int buf = count & 1;
+      // the scales, while the sums are still being made
+      const int64_t row_a0 = (int64_t)(ta * CG + (CG == 2 ? (int)rank : 0)) * 128 + quarter * 32, row_a = row_a0 + lane;
+      const int64_t row_b0 = (int64_t)tb * BN;
+      const float sa = row_a < a.rows_a ? __ldg(a.sa + row_a) : 0.f;
+      float tokens[SWAP ? (BN + 31) / 32 : 1];
+      if constexpr (SWAP) {
+#pragma unroll
+        for (int i = 0; i < (BN + 31) / 32; ++i) tokens[i] = row_b0 + i * 32 + lane < a.rows_b ? __ldg(a.sb + row_b0 + i * 32 + lane) : 0.f;
+      } else {
+#pragma unroll
+        for (int i = 0; i < BN / 32; ++i) {
+          const float f = row_b0 + i * 32 + lane < a.rows_b ? __ldg(a.sb + row_b0 + i * 32 + lane) : 0.f;
+          asm volatile("st.shared.f32 [%0], %1;\n" ::"r"(scales + (uint32_t)(i * 32 + lane) * 4), "f"(f) : "memory");
+        }
+        __syncwarp();
+      }
       if (!mbar_wait(acc_full_bar(buf), (uint32_t)((count >> 1) & 1))) {
         timed_out();
         break;
       }
       asm volatile("tcgen05.fence::after_thread_sync;\n" ::: "memory");
       const uint32_t taddr = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(buf * BN);
-      const int64_t row_a0 = (int64_t)(ta * CG + (CG == 2 ? (int)rank : 0)) * 128 + quarter * 32, row_a = row_a0 + lane;
-      const int64_t row_b0 = (int64_t)tb * BN;
-      const float sa = row_a < a.rows_a ? __ldg(a.sa + row_a) : 0.f;
       T *y = static_cast<T *>(a.y);
       if constexpr (SWAP) {
         // lane = channel, column = token: a warp stores 32 neighbouring channels of a token at a time
@@ -247,7 +318,7 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Ar
           }
           break;   // one tile: the sums meet below
         }
-#pragma unroll 1
+#pragma unroll
         for (int q = 0; q < BN / 16; ++q) {
           if (row_b0 + q * 16 >= a.rows_b) break;
           uint32_t w[16];
@@ -256,7 +327,8 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Ar
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int64_t t = row_b0 + q * 16 + i;
-            if (t < a.rows_b && row_a < a.rows_a) y[t * a.ldy + row_a] = from_f32<T>((float)(int)w[i] * __ldg(a.sb + t) * sa);
+            const float sb = __shfl_sync(0xffffffffu, tokens[q >> 1], (q & 1) * 16 + i);
+            if (t < a.rows_b && row_a < a.rows_a) y[t * a.ldy + row_a] = from_f32<T>((float)(int)w[i] * sb * sa);
           }
         }
       } else {
@@ -277,13 +349,15 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Ar
             asm volatile("tcgen05.wait::ld.sync.aligned;\n" ::: "memory");
 #pragma unroll
             for (int p = 0; p < 32 / kPiece; ++p) {
-              float f[kPiece];
+              float f[kPiece], sb[kPiece];
+#pragma unroll
+              for (int i = 0; i < kPiece; i += 4)
+                asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];\n" : "=f"(sb[i]), "=f"(sb[i + 1]), "=f"(sb[i + 2]), "=f"(sb[i + 3])
+                             : "r"(scales + (uint32_t)(c0 + h * 32 + p * kPiece + i) * 4));
 #pragma unroll
               for (int i = 0; i < kPiece; ++i) {
                 const int c = p * kPiece + i;
-                const int64_t col = col0 + h * 32 + c;
-                const float sb = inside || col < a.rows_b ? __ldg(a.sb + col) : 0.f;
-                f[i] = (float)(int)(c < 16 ? w0[c & 15] : w1[c & 15]) * sa * sb;
+                f[i] = (float)(int)(c < 16 ? w0[c & 15] : w1[c & 15]) * sa * sb[i];
               }
               Chunk<T, kPiece> o;
               o.pack(f);
@@ -340,17 +414,17 @@ __global__ void __launch_bounds__(kInt8Threads, 1) int8_umma_kernel(const Int8Ar
       // Every CTA of the cluster finishes BN / split of the tile's tokens: the others send it their sums for them.
       __syncwarp();
       cluster_sync();   // all MMAs are done and all stages read: the rings may be written
-      const int share = BN / split, row = (warp & 3) * 32 + lane;
-      if (warp >= 4) {
+      const int share_log2 = __ffs(BN / split) - 1, share = 1 << share_log2, row = (warp & 3) * 32 + lane;
+      if (warp >= 4 && warp < 8) {
 #pragma unroll
         for (int c = 0; c < BN; ++c) {
-          const int to = c / share;
-          const uint32_t at = smem0 + (uint32_t)(((int)rank * share + c % share) * 128 + row) * 4;
+          const int to = c >> share_log2;
+          const uint32_t at = smem0 + (uint32_t)(((int)rank * share + (c & (share - 1))) * 128 + row) * 4;
           asm volatile("st.shared::cluster.b32 [%0], %1;\n" ::"r"(map_to_rank(at, (uint32_t)to)), "r"(v[c]) : "memory");
         }
       }
       cluster_sync();
-      if (warp >= 4 && worker < tiles) {
+      if (warp >= 4 && warp < 8 && worker < tiles) {
         int ta, tb;
         place(worker, ta, tb);
         const int64_t o = (int64_t)ta * 128 + row;

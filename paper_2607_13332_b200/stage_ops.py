@@ -30,6 +30,14 @@ def _here(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:
     return t
 
 
+def _pitch(t: torch.Tensor, rows: int, cols: int) -> int:
+    """Leading dimension of a row-major [rows, cols] tensor, in elements."""
+    ld, unit = t.stride()
+    if unit != 1 and cols > 1:
+        raise ValueError("expected a row-major 2-D tensor (unit stride along the last dimension)")
+    return ld if rows > 1 and ld > cols else cols
+
+
 def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) -> int:
     """Address of n contiguous values of that type, or 0."""
     if t is None:
@@ -147,21 +155,23 @@ class QKNormRope:
 # ---- loss against a teacher's top logits --------------------------------------------------------------------------------------
 def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight: Optional[torch.Tensor], temperature: float,
              dlogits: Optional[torch.Tensor], dev_status: Optional[torch.Tensor]) -> torch.Tensor:
-    code = _CODES.get(logits.dtype)
+    dtype = logits.dtype
+    code = _CODES.get(dtype)
     if code is None:
         raise ValueError("logits: expected fp32 or bf16")
-    n, vocab = _here(logits, logits.dtype, "logits").shape
-    if _here(ids, torch.int32, "ids").shape != _here(top, torch.float32, "top").shape or ids.dim() != 2 or ids.shape[0] != n:
+    n, vocab = _here(logits, dtype, "logits").shape
+    rows, top_k = _here(ids, torch.int32, "ids").shape
+    if _here(top, torch.float32, "top").shape != (rows, top_k) or rows != n:
         raise ValueError(f"ids, top: expected [{n}, top_k] each")
     out, ldd = 0, 0
     if dlogits is not None:
-        if _here(dlogits, logits.dtype, "dlogits").shape != logits.shape:
+        if _here(dlogits, dtype, "dlogits").shape != (n, vocab):
             raise ValueError("dlogits: expected the shape of the logits")
-        out, ldd = dlogits.data_ptr(), _ld(dlogits)
+        out, ldd = dlogits.data_ptr(), _pitch(dlogits, n, vocab)
     loss = _new((n,), (1,), torch.float32)
-    st = _lib.stage_distill_loss(logits.data_ptr(), _ld(logits), code, n, vocab, ids.data_ptr(), _ld(ids), top.data_ptr(), _ld(top),
-                                 ids.shape[1], _vector(weight, n, torch.float32, "weight"), temperature, loss.data_ptr(), out, ldd,
-                                 _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
+    st = _lib.stage_distill_loss(logits.data_ptr(), _pitch(logits, n, vocab), code, n, vocab, ids.data_ptr(), _pitch(ids, n, top_k),
+                                 top.data_ptr(), _pitch(top, n, top_k), top_k, _vector(weight, n, torch.float32, "weight"), temperature,
+                                 loss.data_ptr(), out, ldd, _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
     if st:
         binding.check(st, "stage_distill_loss")
     return loss
@@ -179,8 +189,8 @@ def distill_loss_grad(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor
     """distill_loss and the gradient of its sum with respect to the logits, in one pass: (loss, dlogits).  dlogits may be the
     logits; made here, it has the logits' leading dimension."""
     if dlogits is None:
-        ld = _ld(_here(logits, logits.dtype, "logits"))
-        dlogits = _new(tuple(logits.shape), (ld, 1), logits.dtype)
+        n, vocab = logits.shape
+        dlogits = _new((n, vocab), (_pitch(_here(logits, logits.dtype, "logits"), n, vocab), 1), logits.dtype)
     return _distill(logits, ids, top, weight, temperature, dlogits, dev_status), dlogits
 
 
@@ -193,14 +203,14 @@ def int8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None):
         raise ValueError("x: expected fp32 or bf16")
     rows, cols = _here(x, x.dtype, "x").shape
     if q is None:
-        ldq = -(-cols // 16) * 16
+        ldq = cols + (-cols & 15)
         q = _new((rows, cols), (ldq, 1), torch.int8)
-    elif _here(q, torch.int8, "q").shape != x.shape:
+    elif _here(q, torch.int8, "q").shape != (rows, cols):
         raise ValueError("q: expected the shape of x")
     else:
-        ldq = _ld(q)
+        ldq = _pitch(q, rows, cols)
     scale = _new((rows,), (1,), torch.float32)
-    st = _lib.stage_int8_quantize(x.data_ptr(), _ld(x), code, rows, cols, q.data_ptr(), ldq, scale.data_ptr(), _stream())
+    st = _lib.stage_int8_quantize(x.data_ptr(), _pitch(x, rows, cols), code, rows, cols, q.data_ptr(), ldq, scale.data_ptr(), _stream())
     if st:
         binding.check(st, "stage_int8_quantize")
     return q, scale
@@ -213,15 +223,16 @@ def int8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.
     outer, depth = _here(wq, torch.int8, "wq").shape
     if depth != inner:
         raise ValueError(f"wq: expected [outer, {inner}]")
+    kind = _TORCH_DTYPE[dtype]
     if out is None:
-        out, ldy = _new((n, outer), (outer, 1), _TORCH_DTYPE[dtype]), outer
-    elif _here(out, _TORCH_DTYPE[dtype], "out").shape != (n, outer):
+        out, ldy = _new((n, outer), (outer, 1), kind), outer
+    elif _here(out, kind, "out").shape != (n, outer):
         raise ValueError(f"out: expected [{n}, {outer}]")
     else:
-        ldy = _ld(out)
-    st = _lib.stage_int8_matmul(xq.data_ptr(), _ld(xq), _vector(xs, n, torch.float32, "xs"), wq.data_ptr(), _ld(wq),
-                                _vector(ws, outer, torch.float32, "ws"), n, inner, outer, out.data_ptr(), ldy, binding.DTYPES[dtype],
-                                _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
+        ldy = _pitch(out, n, outer)
+    st = _lib.stage_int8_matmul(xq.data_ptr(), _pitch(xq, n, inner), _vector(xs, n, torch.float32, "xs"), wq.data_ptr(),
+                                _pitch(wq, outer, inner), _vector(ws, outer, torch.float32, "ws"), n, inner, outer, out.data_ptr(), ldy,
+                                _CODES[kind], _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
     if st:
         binding.check(st, "stage_int8_matmul")
     return out
