@@ -79,7 +79,8 @@ ssn_status_t stage_qk_rope_forward(const stage_qk_rope_t *op, const void *q, int
  *   q, k            the forward INPUTS
  *   dq_in, dk_in    out, gradients of the inputs; may be dq / dk (same address and strides)
  *   dwq, dwk        out, fp32 [D] each, overwritten (zeros when there are no rows), or NULL: not wanted
- *   workspace       of stage_qk_rope_workspace_bytes(), 16-byte aligned; not needed when dwq and dwk are NULL
+ *   workspace       of stage_qk_rope_workspace_bytes(), 16-byte aligned; not needed when dwq and dwk are NULL.  The size is the
+ *                   same for every n_tokens > 0; calls that may run at one time need one each
  */
 size_t stage_qk_rope_workspace_bytes(const stage_qk_rope_t *op, int64_t n_tokens, int32_t q_heads, int32_t k_heads);
 ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, int64_t dq_token, int64_t dq_head,
@@ -101,7 +102,7 @@ ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, i
  * With x = logits[t] / tau over the vocabulary and p the softmax of top[t] / tau over the row's entries,
  *     loss[t]       = weight[t] tau^2 sum_j p_j (log p_j - x[ids[t, j]] + log sum_v exp x_v)
  *     dlogits[t, v] = weight[t] tau (softmax(x)_v - sum over the j with ids[t, j] = v of p_j)
- *   logits   [n_tokens x vocab] of dtype, ldl >= vocab
+ *   logits   [n_tokens x vocab] of dtype, ldl >= vocab, vocab <= 2^31 - 16
  *   ids      int32 [n_tokens x top_k], ldi >= top_k, and top, fp32 [n_tokens x top_k], ldt >= top_k: the row's
  *            entries in any order, 1 <= top_k <= STAGE_DISTILL_MAX_TOP.  An id of -1 is padding; any other id outside
  *            [0, vocab) ORs SSN_DEV_BAD_ID into *dev_status and counts as padding.  An id may stand there twice.
@@ -139,8 +140,9 @@ ssn_status_t stage_int8_quantize(const void *x, int64_t ldx, int32_t dtype, int6
  *   xq  int8 [n_tokens x inner], ldx >= inner;  xs  fp32 [n_tokens];  wq  int8 [outer x inner], ldw >= inner;
  *   ws  fp32 [outer];  y  [n_tokens x outer] of dtype, ldy >= outer;  1 <= inner <= STAGE_INT8_MAX_INNER
  *   dev_status  device int32 or NULL: SSN_DEV_TIMEOUT when an internal bounded wait ran out (y is invalid then)
- * Any int8 value may occur, -128 too.  xq and wq rows that start on 16-byte boundaries (address and leading dimension)
- * are fetched by TMA; others take a slower kernel.
+ * Any int8 value may occur, -128 too.  Rows that start on 16-byte boundaries (address and leading dimension of xq and wq) are
+ * fetched by TMA; with others the product takes about five times as long.  Any y will do; rows on 16-byte boundaries are
+ * stored 16 bytes at a time.
  */
 ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, const int8_t *wq, int64_t ldw,
                                const float *ws, int64_t n_tokens, int64_t inner, int64_t outer, void *y, int64_t ldy,

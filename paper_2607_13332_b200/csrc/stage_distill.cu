@@ -4,11 +4,12 @@
 // the gradient is w tau exp((s - m) / tau) / L, minus w tau p at the teacher's ids.  The loss reads the row once; the
 // gradient reads it once more out of L2 and writes it once, so that HBM sees the row read once and written once.
 //
-// What bounds it: HBM for the loss of long rows (2048 x 128256 bf16 in 101 us, 5.2 TB/s).  The gradient (8192 x 128256 bf16 in
-// 0.99 ms, 4.2 TB/s) also waits for its exponentials, two per element on a pipe of 16 lanes per clock and SM (58 % busy), and
-// for the reductions between the passes.  Tried and dropped: the exponentials of a row kept in the registers of a cluster of
-// eight CTAs, so that each is computed once (1.44 ms: 33 of the 37 clusters fit, and 20 warps share too little of a row);
-// a ring of bulk copies with a warp of its own (1.01 ms); registers filled a round ahead (slower, fewer warps).
+// What bounds it: HBM for the loss of long rows (2048 x 128256 bf16 in 96 us, 5.5 TB/s).  The gradient (8192 x 128256 bf16 in
+// 0.95 ms, 4.4 TB/s) also waits for its exponentials, two per element on a pipe of 16 lanes per clock and SM, and for the
+// reductions between the passes.  Tried and dropped: the exponentials of a row kept in the registers of a cluster of eight
+// CTAs, so that each is computed once (1.44 ms: 33 of the 37 clusters fit, and 20 warps share too little of a row); a ring of
+// bulk copies with a warp of its own (1.01 ms); registers filled a round ahead (fewer warps, slower); bf16 widened by shifts
+// before the subtraction (1.01 against 0.96 ms with four pieces in flight).
 //
 // Sums are fp32 per thread, relative to the thread's running maximum, then over warps and CTAs in a fixed order; the loss
 // itself, a difference of large terms, is put together in 64 bits.
@@ -60,10 +61,6 @@ __device__ __forceinline__ MaxSum merge_warp(MaxSum ms, float scale) {
   return {m, l};
 }
 
-__device__ __forceinline__ float2 exponents(float2 s, float base, float scale) {
-  return mul2(add2(s, make_float2(-base, -base)), make_float2(scale, scale));
-}
-
 // 16 bytes of a row
 template <typename T> struct Piece {
   static constexpr int E = 16 / (int)sizeof(T), kPairs = E / 2;
@@ -94,7 +91,15 @@ template <typename T> struct Piece {
     for (int i = 0; i < E; ++i)
       if (first + i >= 0 && first + i < vocab) row[first + i] = from_f32<T>(c.get(i));   // exact: it was rounded when packed
   }
-  __device__ __forceinline__ float2 pair(int i) const { return make_float2(c.get(2 * i), c.get(2 * i + 1)); }
+  // (s - base) scale of the pair i; a bf16 is widened by the subtraction itself
+  __device__ __forceinline__ float2 exponents(int i, float base, float scale) const {
+    float2 d;
+    if constexpr (sizeof(T) == 2)
+      asm("{\n.reg .b16 l, h;\nmov.b32 {l, h}, %2;\nsub.rn.f32.bf16 %0, l, %3;\nsub.rn.f32.bf16 %1, h, %3;\n}\n" : "=f"(d.x), "=f"(d.y) : "r"(c.raw.v[i]), "f"(base));
+    else
+      d = add2(make_float2(c.get(2 * i), c.get(2 * i + 1)), make_float2(-base, -base));
+    return mul2(d, make_float2(scale, scale));
+  }
   __device__ __forceinline__ float largest() const {
     if constexpr (sizeof(T) == 4) {
       return fmaxf(fmaxf(c.get(0), c.get(1)), fmaxf(c.get(2), c.get(3)));
@@ -107,7 +112,7 @@ template <typename T> struct Piece {
   __device__ __forceinline__ float2 sum_exp(float2 l, float base, float scale) const {
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-      const float2 y = exponents(pair(i), base, scale);
+      const float2 y = exponents(i, base, scale);
       l = add2(l, make_float2(exp2_approx(y.x), exp2_approx(y.y)));
     }
     return l;
@@ -116,7 +121,7 @@ template <typename T> struct Piece {
     float g[E];
 #pragma unroll
     for (int i = 0; i < kPairs; ++i) {
-      const float2 y = exponents(pair(i), base, scale);
+      const float2 y = exponents(i, base, scale);
       const float2 z = mul2(make_float2(exp2_approx(y.x), exp2_approx(y.y)), make_float2(c_, c_));
       g[2 * i] = z.x;
       g[2 * i + 1] = z.y;
@@ -141,8 +146,8 @@ struct Teacher {
   double a;
 };
 
-// Resident CTAs of `threads`: 64 registers per thread for the gradient, 48 for the loss
-constexpr int per_sm(int threads, bool grad) { return (grad ? 1024 : 1280) / threads; }
+// Resident CTAs of `threads`: what leaves the pieces in flight in registers
+constexpr int per_sm(int threads, bool grad) { return threads == 256 ? (grad ? 3 : 4) : (grad ? 8 : 10); }
 
 struct __align__(16) Part {   // one CTA's share of a row
   double a;
@@ -165,7 +170,7 @@ struct Shared {
 // pieces, so that their latency passes behind the row.
 template <typename T, int kThreads, bool GRAD>
 __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kernel(const __grid_constant__ DistillArgs a) {
-  constexpr int E = Piece<T>::E, U = 4, kWarps = kThreads / 32;   // U pieces in flight per thread
+  constexpr int E = Piece<T>::E, U = kThreads == 256 ? 6 : 4, kWarps = kThreads / 32;   // U pieces in flight per thread
   __shared__ Shared sh;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint32_t cluster, rank;
@@ -380,8 +385,8 @@ template <typename T, int kThreads, bool GRAD> cudaError_t launch_threads(const 
 
 // Threads per CTA by the row's bytes: a row costs a CTA a few microseconds besides its bytes, which more CTAs per SM hide, while
 // long rows want fewer of them (the second pass finds its row in L2).  0.5 GB of logits in rows of 64 / 130 / 256 KB, with the
-// gradient: 128 threads 254 / 276 / 292 us, 256 threads 287 / 246 / 269; the loss alone 104 / 103 / 109 and 130 / 104 / 101.
-// 512 threads would take the longest rows' gradient in 245, but the loss alone in 113; both calls add a row up in the same
+// gradient: 128 threads 254 / 276 / 292 us, 256 threads 287 / 246 / 269; the loss alone 104 / 103 / 109 and 130 / 104 / 101.  (With six
+// pieces in flight instead of four, 256 threads take another tenth off rows of 256 KB.)  Both calls add a row up in the same
 // order, so that its loss is the same number with the gradient and without.
 template <typename T> cudaError_t launch_distill(const DistillArgs &a, cudaStream_t stream) {
   const bool many = a.vocab * (int64_t)sizeof(T) >= 98304;
@@ -399,7 +404,7 @@ extern "C" ssn_status_t stage_distill_loss(const void *logits, int64_t ldl, int3
                                            const float *weight, float tau, float *loss, void *dlogits, int64_t ldd,
                                            int32_t *dev_status, void *stream) {
   if (dtype != SSN_F32 && dtype != SSN_BF16) return SSN_ERR_DTYPE;
-  if (n_tokens < 0 || vocab < 1 || vocab > 0x7fffffffLL || top_k < 1 || top_k > STAGE_DISTILL_MAX_TOP) return SSN_ERR_SHAPE;
+  if (n_tokens < 0 || vocab < 1 || vocab > 0x7ffffff0LL || top_k < 1 || top_k > STAGE_DISTILL_MAX_TOP) return SSN_ERR_SHAPE;
   if (ldl < vocab || ldi < top_k || ldt < top_k || (dlogits != nullptr && ldd < vocab)) return SSN_ERR_SHAPE;
   if (!(tau >= STAGE_DISTILL_MIN_TAU && tau <= STAGE_DISTILL_MAX_TAU)) return SSN_ERR_SHAPE;
   if (n_tokens == 0) return SSN_OK;

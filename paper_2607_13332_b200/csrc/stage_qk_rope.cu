@@ -93,11 +93,11 @@ template <typename T, int V, bool ADJ> struct Unit {
 };
 
 // Copies a piece to shared memory behind this thread's back; two bytes are more than cp.async can (they wait here)
-template <int BYTES> __device__ __forceinline__ void copy_piece(unsigned char *to, const void *from) {
-  const uint32_t at = smem_address(to);
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(at), "l"(from) : "memory");
-  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
-  else *reinterpret_cast<uint16_t *>(to) = *static_cast<const uint16_t *>(from);
+template <int BYTES> __device__ __forceinline__ void copy_piece(unsigned char *to, const void *from, bool there = true) {
+  const uint32_t at = smem_address(to), bytes = there ? BYTES : 0;   // the rest becomes zeros
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(at), "l"(from), "r"(bytes) : "memory");
+  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(at), "l"(from), "n"(BYTES), "r"(bytes) : "memory");
+  else *reinterpret_cast<uint16_t *>(to) = there ? *static_cast<const uint16_t *>(from) : (uint16_t)0;
 }
 
 __device__ __forceinline__ float group_sum(float x, int group_log2) {
@@ -110,7 +110,7 @@ __device__ __forceinline__ float group_sum(float x, int group_log2) {
 // NU units per lane (more than one only where V is small).  A warp's rows come through a ring in shared memory: every lane
 // copies its own pieces kAhead passes ahead (cp.async, no registers held), and the warp together the table rows of the tokens
 // that these passes begin.
-template <typename T, int V, int NU, bool ADJ, bool BACK>
+template <typename T, int V, int NU, bool ADJ, bool BACK, bool FULL>
 __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int P = BACK ? kBackAhead : kForwardAhead, kPieceBytes = V * (int)sizeof(T), kUnitBytes = 2 * 32 * kPieceBytes;
   constexpr int kPassBytes = (BACK ? 2 : 1) * NU * kUnitBytes, kTables = P + 1;
@@ -133,8 +133,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
 #pragma unroll
   for (int n = 0; n < NU; ++n) {
     pair[n] = (unit0 + (n << lg)) * V;
-    mine[n] = 2 * pair[n] < a.d;
-    turned[n] = pair[n] < half;
+    mine[n] = FULL || 2 * pair[n] < a.d;
+    turned[n] = FULL || pair[n] < half;   // FULL: every column turns
     if (ADJ) {
       at0[n] = 2 * pair[n];
       at1[n] = at0[n] + V;
@@ -194,18 +194,18 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
         ahead_t += slots;
         if (ahead_t < a.n) ahead_pos = table_row(a, ahead_t);   // known when that token begins
       }
-      if (ahead_row < heads) {
-        unsigned char *to = ring + ahead_place + lane * kPieceBytes;
+      // a row past the last head, or a unit past D, becomes zeros: it adds nothing to a sum
+      unsigned char *to = ring + ahead_place + lane * kPieceBytes;
 #pragma unroll
-        for (int n = 0; n < NU; ++n)
-          if (mine[n]) {
-            copy_piece<kPieceBytes>(to + n * kUnitBytes, x + at0[n]);
-            copy_piece<kPieceBytes>(to + n * kUnitBytes + 32 * kPieceBytes, x + at1[n]);
-            if (BACK) {
-              copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes, dy + at0[n]);
-              copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes + 32 * kPieceBytes, dy + at1[n]);
-            }
-          }
+      for (int n = 0; n < NU; ++n) {
+        const bool there = mine[n] && ahead_row < heads;
+        const T *from = there ? x : static_cast<const T *>(s.x), *from_dy = BACK ? there ? dy : static_cast<const T *>(s.dy) : nullptr;
+        copy_piece<kPieceBytes>(to + n * kUnitBytes, from + (there ? at0[n] : 0), there);
+        copy_piece<kPieceBytes>(to + n * kUnitBytes + 32 * kPieceBytes, from + (there ? at1[n] : 0), there);
+        if (BACK) {
+          copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes, from_dy + (there ? at0[n] : 0), there);
+          copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes + 32 * kPieceBytes, from_dy + (there ? at1[n] : 0), there);
+        }
       }
       ahead_row += rows_per_pass;
       x += x_step;
@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
       const float *cs = tables + table * table_floats;
 #pragma unroll
       for (int n = 0; n < NU; ++n)
-        if (mine[n] && turned[n]) {
+        if (turned[n] && (FULL ? NU == 1 || mine[n] : mine[n])) {
           float c[V], sn[V];
 #pragma unroll
           for (int i = 0; i < V; ++i) c[i] = cs[pair[n] + i], sn[i] = cs[half + pair[n] + i];
@@ -259,12 +259,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
 #pragma unroll
     for (int n = 0; n < NU; ++n) {
       Unit<T, V, ADJ> u;
-      if (mine[n] && there) {
-        u.take(place + n * kUnitBytes);
-      } else {   // zeros: they add nothing to a sum
-        const float zero[V] = {};
-        u.pack(zero, zero);
-      }
+      u.take(place + n * kUnitBytes);
       u.get(xa[n], xb[n]);
       v_fma(sq, xa[n], xa[n], sq);
       v_fma(sq, xb[n], xb[n], sq);
@@ -291,12 +286,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
 #pragma unroll
       for (int n = 0; n < NU; ++n) {
         Unit<T, V, ADJ> u;
-        if (mine[n] && there) {
-          u.take(place + (NU + n) * kUnitBytes);
-        } else {
-          const float zero[V] = {};
-          u.pack(zero, zero);
-        }
+        u.take(place + (NU + n) * kUnitBytes);
         float ga[V], gb[V];
         u.get(ga, gb);
         if (turned[n]) {
@@ -470,12 +460,12 @@ int side_blocks(int sms, int per_sm, int32_t heads, int32_t other, int rows_per_
   return b < 1 ? 1 : (int)b;
 }
 
-template <typename T, int V, int NU, bool ADJ, bool BACK>
+template <typename T, int V, int NU, bool ADJ, bool BACK, bool FULL = false>
 cudaError_t launch_unit(const RopeArgs &a, cudaStream_t stream) {
   static std::atomic<uint64_t> allowed{0};
   constexpr int P = BACK ? kBackAhead : kForwardAhead;
   constexpr int kRing = kWarps * P * (BACK ? 2 : 1) * NU * 2 * 32 * V * (int)sizeof(T);
-  auto kernel = qk_rope_kernel<T, V, NU, ADJ, BACK>;
+  auto kernel = qk_rope_kernel<T, V, NU, ADJ, BACK, FULL>;
   const cudaError_t e = allow_dynamic_smem(kernel, kRing + kWarps * (P + 1) * STAGE_MAX_HEAD_DIM * 4, allowed);
   if (e != cudaSuccess) return e;
   return launch_dependent(kernel, (unsigned)(a.side[0].blocks + a.side[1].blocks), kThreads, kRing + kWarps * (P + 1) * a.table_bytes, stream, 1, a);
@@ -483,6 +473,9 @@ cudaError_t launch_unit(const RopeArgs &a, cudaStream_t stream) {
 
 template <typename T, bool ADJ, bool BACK>
 cudaError_t launch_width(const RopeArgs &a, int v, cudaStream_t stream) {
+  // whole heads that turn, with as many units as lanes, are the common case: they need no choices
+  constexpr int kWide = 16 / (int)sizeof(T);
+  if (v == kWide && a.rot == a.d && (a.d / (2 * kWide) & (a.d / (2 * kWide) - 1)) == 0) return launch_unit<T, kWide, 1, ADJ, BACK, true>(a, stream);
   if constexpr (sizeof(T) == 2) {
     if (v == 8) return launch_unit<T, 8, 1, ADJ, BACK>(a, stream);
   }

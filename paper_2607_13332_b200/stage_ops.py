@@ -73,6 +73,7 @@ class QKNormRope:
         self.c = binding.make_qk_rope(head_dim, rot, binding.DTYPES[dtype], binding.PAIRINGS[pairing], eps, _ptr(wq), _ptr(wk),
                                       _ptr(table), _ld(table) if table is not None else 0, max_pos, self.dev_status.data_ptr())
         self._ref = byref(self.c)
+        self._workspace = {}
 
     def take_status(self) -> int:
         """Read and clear the device status word (synchronises): SSN_DEV_BAD_POS of every call since the last read."""
@@ -142,7 +143,9 @@ class QKNormRope:
         nbytes = 0
         if gains:
             d = self.head_dim
-            nbytes = _lib.stage_qk_rope_workspace_bytes(self._ref, n, qh, kh)
+            nbytes = self._workspace.get((qh, kh))      # does not depend on the number of tokens
+            if nbytes is None:
+                nbytes = self._workspace[qh, kh] = _lib.stage_qk_rope_workspace_bytes(self._ref, 1, qh, kh)
             dwq, dwk = _new((d,), (1,), torch.float32), _new((d,), (1,), torch.float32)
             scratch = _new((nbytes,), (1,), torch.uint8)      # one per call: captured calls share none
         st = _lib.stage_qk_rope_backward(self._ref, *dqa, *dka, *qa, qh, *ka, kh, *dqo, *dko, _ptr(dwq), _ptr(dwk),
