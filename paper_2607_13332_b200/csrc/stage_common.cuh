@@ -93,6 +93,13 @@ template <typename T, int V> __device__ __forceinline__ void Chunk<T, V>::pack(c
   }
 }
 
+// The larger one, a NaN if either is one
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+
 // Two fp32 values per instruction
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
   float2 d;

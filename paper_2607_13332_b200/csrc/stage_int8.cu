@@ -32,12 +32,6 @@ __device__ __forceinline__ int quantised_small(float x, float s) {
 }
 constexpr float kSmallScale = 1e-30f;
 
-// The larger one, a NaN if either is one
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float m;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-  return m;
-}
 // The row's scale from its largest magnitude, 0 for a row with a value that is not finite, and an approximate reciprocal
 __device__ __forceinline__ bool scale_of(float top, float &s, float &inv) {
   const bool fine = top < INFINITY;
@@ -190,7 +184,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) int8_few_kernel(const Int8Matm
   int acc[N][kChannels] = {};
   const int pieces = (int)((a.inner + 15) / 16), last = (int)(a.inner & 15);
   auto fetch = [&](const int8_t *row, int piece) {
-    if (ANYWHERE) return load_row16(row, piece * 16, (int)a.inner);
+    if (ANYWHERE) return row16(fetch_row16(row, piece * 16, (int)a.inner), row, piece * 16, (int)a.inner);
     const uint4 v = __ldg(reinterpret_cast<const uint4 *>(row) + piece);
     return piece == pieces - 1 && last != 0 ? first_bytes(v, last) : v;
   };

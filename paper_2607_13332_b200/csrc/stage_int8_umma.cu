@@ -1,6 +1,8 @@
 // Dispatch of the tcgen05 8-bit product (see stage_int8_umma.cuh).
 #include "stage_int8_umma.cuh"
 
+#include <algorithm>
+
 #include "codec_tensor_maps.h"
 
 namespace ssn {
@@ -40,24 +42,26 @@ cudaError_t launch_tiles(const Int8Matmul &m, int split, int sm_count, cudaStrea
   return launch_dependent(kernel, (unsigned)(workers * cluster), Cfg::kThreads, Cfg::kSmemBytes, stream, cluster, a, maps);
 }
 
-// CTAs per tile of 128 channels, while there are SMs for them and each keeps a few steps of the inner dimension
-int split_of(const Int8Matmul &m, int sms) {
-  const int64_t steps = (m.inner + kInt8Step - 1) / kInt8Step, tiles = (m.outer + 127) / 128;
+// CTAs per tile of 128 channels x bn tokens, while there are SMs for them and each keeps a few steps of the inner dimension.  Not
+// every SM of a GPC is in a cluster: a sixteenth cluster of eight would run after the others (100 x 4096 x 1024: 17.8 us).
+int split_of(const Int8Matmul &m, int bn, int sms) {
+  const int64_t steps = (m.inner + kInt8Step - 1) / kInt8Step, tiles = (m.outer + 127) / 128 * ((m.n + bn - 1) / bn);
   int split = 1;
-  while (split < 8 && tiles * split * 2 <= sms && steps >= split * 4) split *= 2;
+  while (split < 8 && tiles * split * 2 <= (split == 4 ? sms * 13 / 16 : sms * 7 / 8) && steps >= split * 4) split *= 2;
   return split;
 }
 
 template <typename T> cudaError_t launch_ragged(const Int8Matmul &m, int sms, cudaStream_t stream) {
-  if (m.n <= 16) return launch_tiles<1, 16, true, T, true>(m, split_of(m, sms), sms, stream);
-  if (m.n <= 64) return launch_tiles<1, 64, true, T, true>(m, split_of(m, sms), sms, stream);
+  if (m.n <= 16) return launch_tiles<1, 16, true, T, true>(m, split_of(m, 16, sms), sms, stream);
+  const int split = split_of(m, 64, sms);   // few tiles: several CTAs for each
+  if (m.n <= 64 || split > 1) return launch_tiles<1, 64, true, T, true>(m, split, sms, stream);
   return launch_tiles<1, 128, false, T, true>(m, 1, sms, stream);
 }
 
 template <typename T> cudaError_t launch_typed(const Int8Matmul &m, int sms, cudaStream_t stream) {
-  if (m.n <= 16) return launch_tiles<1, 16, true, T>(m, split_of(m, sms), sms, stream);
-  if (m.n <= 32) return launch_tiles<1, 32, true, T>(m, split_of(m, sms), sms, stream);
-  if (m.n <= 64) return launch_tiles<1, 64, true, T>(m, split_of(m, sms), sms, stream);
+  if (m.n <= 16) return launch_tiles<1, 16, true, T>(m, split_of(m, 16, sms), sms, stream);
+  if (m.n <= 32) return launch_tiles<1, 32, true, T>(m, split_of(m, 32, sms), sms, stream);
+  if (m.n <= 64) return launch_tiles<1, 64, true, T>(m, split_of(m, 64, sms), sms, stream);
   // The shape whose waves of tiles take the least time: a step of a wave of pairs of 256 x 256 takes about 0.38 us, of CTAs of
   // 128 x 256 0.42 (each loads B for itself), of the narrower ones 0.26; a wave's first loads and a tile's output cost as much as
   // some 8 and 5 steps.  Measured (us; pairs 256, pairs 128, CTAs 256, CTAs 128): 777 x 2000 x 5003 22.8 / 22.9 / 18.0 / 20.2,
@@ -69,6 +73,8 @@ template <typename T> cudaError_t launch_typed(const Int8Matmul &m, int sms, cud
   };
   const int64_t half = (m.n + 127) / 128, whole = (m.n + 255) / 256;
   const double pairs = time(whole, 256, sms / 2, 0.38, 4.0), wide = time(half, 256, sms, 0.42, 3.5), narrow = time(half, 128, sms, 0.28, 3.0);
+  const int split = split_of(m, 64, sms);   // few tiles: several CTAs for each
+  if (split > 1 && steps / split * 0.2 + 7.0 < std::min(pairs, std::min(wide, narrow))) return launch_tiles<1, 64, true, T>(m, split, sms, stream);
   if (wide < pairs && wide <= narrow) return launch_tiles<1, 256, false, T>(m, 1, sms, stream);
   if (narrow < pairs) return launch_tiles<1, 128, false, T>(m, 1, sms, stream);
   return launch_tiles<2, 256, false, T>(m, 1, sms, stream);

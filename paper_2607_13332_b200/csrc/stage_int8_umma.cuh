@@ -163,23 +163,33 @@ int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
     for (int64_t tile = worker; tile < tiles && !dead; tile += workers) {
       int ta, tb;
       place(tile, ta, tb);
-      uint4 v[kPerThread], next[kPerThread];
-      auto fetch = [&](uint4 (&to)[kPerThread], int st) {
+      Row16 next[kPerThread];
+      auto row_of = [&](int i, int &bytes) {   // row i of this thread; one past the operand's end has no bytes
+        const int r = row0 + i * kRowStep;
+        const bool is_a = r < 128;
+        const int64_t row = is_a ? (int64_t)ta * 128 + r : (int64_t)tb * BN + r - 128;
+        const bool there = r < kRows && row < (is_a ? a.rows_a : a.rows_b);
+        bytes = there ? a.inner : 0;
+        return (is_a ? a.a : a.b) + (there ? row : 0) * (is_a ? a.lda : a.ldb);
+      };
+      auto fetch = [&](int st) {
 #pragma unroll
         for (int i = 0; i < kPerThread; ++i) {
-          const int r = row0 + i * kRowStep;
-          const bool is_a = r < 128;
-          const int64_t row = is_a ? (int64_t)ta * 128 + r : (int64_t)tb * BN + r - 128;
-          to[i] = make_uint4(0, 0, 0, 0);
-          if (r < kRows && row < (is_a ? a.rows_a : a.rows_b))
-            to[i] = load_row16(is_a ? a.a + row * a.lda : a.b + row * a.ldb, st * kInt8Step + piece * 16, a.inner);
+          int bytes;
+          const int8_t *row = row_of(i, bytes);
+          next[i] = fetch_row16(row, st * kInt8Step + piece * 16, a.inner);
         }
       };
-      fetch(next, step_lo);
+      fetch(step_lo);
       for (int st = step_lo; st < step_hi; ++st) {
+        uint4 v[kPerThread];
 #pragma unroll
-        for (int i = 0; i < kPerThread; ++i) v[i] = next[i];
-        if (st + 1 < step_hi) fetch(next, st + 1);   // on its way while this one is stored
+        for (int i = 0; i < kPerThread; ++i) {
+          int bytes;
+          const int8_t *row = row_of(i, bytes);
+          v[i] = row16(next[i], row, st * kInt8Step + piece * 16, bytes);
+        }
+        if (st + 1 < step_hi) fetch(st + 1);   // on its way while this one is stored
         if (!dead && !mbar_wait(empty_bar(slot), parity)) {
           timed_out();
           break;
