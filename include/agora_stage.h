@@ -12,7 +12,8 @@
  * ELEMENTS, nothing allocated, freed or synchronised inside, work enqueued on `stream` (a cudaStream_t
  * passed as void*) of the current device, host-detectable mistakes refused before a launch, one
  * element type (ssn_dtype_t) per call unless stated, sums in fp32 or wider and ONE rounding at the end.
- * Buffers of one call must not overlap unless stated.  A call's result is the same bits every time.
+ * Buffers of one call must not overlap unless stated; each is aligned to its element (SSN_ERR_SHAPE if not).  A call's
+ * result is the same bits every time.
  */
 #ifndef AGORA_STAGE_H_
 #define AGORA_STAGE_H_

@@ -4,7 +4,7 @@
 // the gradient is w tau exp((s - m) / tau) / L, minus w tau p at the teacher's ids.  The loss reads the row once; the
 // gradient reads it once more out of L2 and writes it once, so that HBM sees the row read once and written once.
 //
-// What bounds it: HBM for the loss of long rows (2048 x 128256 bf16 in 96 us, 5.5 TB/s).  The gradient (8192 x 128256 bf16 in
+// What bounds it: HBM for the loss of long rows (2048 x 128256 bf16 in 100 us, 5.2 TB/s).  The gradient (8192 x 128256 bf16 in
 // 0.95 ms, 4.4 TB/s) also waits for its exponentials, two per element on a pipe of 16 lanes per clock and SM, and for the
 // reductions between the passes.  Tried and dropped: the exponentials of a row kept in the registers of a cluster of eight
 // CTAs, so that each is computed once (1.44 ms: 33 of the 37 clusters fit, and 20 warps share too little of a row); a ring of
@@ -414,6 +414,8 @@ extern "C" ssn_status_t stage_distill_loss(const void *logits, int64_t ldl, int3
   if (logits == nullptr || ids == nullptr || top == nullptr || loss == nullptr) return SSN_ERR_NULL;
   const size_t item = dtype == SSN_F32 ? 4 : 2;
   if (!aligned_to(logits, item) || !aligned_to(dlogits, item)) return SSN_ERR_SHAPE;
+  for (const void *p : {(const void *)ids, (const void *)top, (const void *)weight, (const void *)loss, (const void *)dev_status})
+    if (!aligned_to(p, 4)) return SSN_ERR_SHAPE;
   if (dlogits == logits && ldd != ldl) return SSN_ERR_SHAPE;
   const DistillArgs a{logits, dlogits, ids, top, weight, loss, dev_status, ldl, ldd, ldi, ldt, n_tokens, vocab, top_k, tau};
   cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -252,7 +252,7 @@ ssn_status_t stage_int8_quantize(const void *x, int64_t ldx, int32_t dtype, int6
   const int64_t far = ((int64_t)1 << 60) / rows;
   if (ldx > far || ldq > far) return SSN_ERR_SHAPE;
   if (x == nullptr || q == nullptr || scale == nullptr) return SSN_ERR_NULL;
-  if (!aligned_to(x, dtype == SSN_F32 ? 4 : 2)) return SSN_ERR_SHAPE;
+  if (!aligned_to(x, dtype == SSN_F32 ? 4 : 2) || !aligned_to(scale, 4)) return SSN_ERR_SHAPE;
   const QuantArgs a{x, q, scale, ldx, ldq, rows, cols};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   return launched(dtype == SSN_F32 ? launch_quantize<float>(a, s) : launch_quantize<__nv_bfloat16>(a, s));
@@ -269,7 +269,7 @@ ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, c
   constexpr int64_t kFar = (int64_t)1 << 60;
   if (ldx > kFar / n_tokens || ldy > kFar / n_tokens || ldw > kFar / outer || n_tokens > kFar / outer) return SSN_ERR_SHAPE;
   if (xq == nullptr || xs == nullptr || wq == nullptr || ws == nullptr || y == nullptr) return SSN_ERR_NULL;
-  if (!aligned_to(y, dtype == SSN_F32 ? 4 : 2)) return SSN_ERR_SHAPE;
+  if (!aligned_to(y, dtype == SSN_F32 ? 4 : 2) || !aligned_to(xs, 4) || !aligned_to(ws, 4) || !aligned_to(dev_status, 4)) return SSN_ERR_SHAPE;
   const Int8Matmul given{xq, wq, xs, ws, y, ldx, ldw, ldy, n_tokens, inner, outer, dev_status};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   // the pitch of a single row does not matter

@@ -405,8 +405,10 @@ ssn_status_t check_op(const stage_qk_rope_t *op) {
   if (!(op->eps >= 0.f) || std::isinf(op->eps)) return SSN_ERR_SHAPE;
   if (op->rot_dim > 0) {
     if (op->table == nullptr) return SSN_ERR_NULL;
-    if (op->ldt < op->rot_dim || op->max_pos < 1) return SSN_ERR_SHAPE;
+    if (op->ldt < op->rot_dim || op->max_pos < 1 || !aligned_to(op->table, 4)) return SSN_ERR_SHAPE;
   }
+  const size_t item = op->dtype == SSN_F32 ? 4 : 2;
+  if (!aligned_to(op->wq, item) || !aligned_to(op->wk, item) || !aligned_to(op->dev_status, 4)) return SSN_ERR_SHAPE;
   return SSN_OK;
 }
 
@@ -552,6 +554,7 @@ ssn_status_t stage_rope_table(float *table, int64_t ldt, int32_t max_pos, int32_
   if (rot_dim < 2 || (rot_dim & 1) || max_pos < 0 || ldt < rot_dim || !(theta > 0.0) || std::isinf(theta)) return SSN_ERR_SHAPE;
   if (max_pos == 0) return SSN_OK;
   if (table == nullptr) return SSN_ERR_NULL;
+  if (!aligned_to(table, 4)) return SSN_ERR_SHAPE;
   const int64_t blocks = ((int64_t)max_pos * (rot_dim / 2) + 255) / 256, cap = (int64_t)stage_sm_count() * 8;
   return launched(launch_dependent(rope_table_kernel, (unsigned)(blocks < cap ? blocks : cap), 256, 0, static_cast<cudaStream_t>(stream), 1,
                                    table, ldt, max_pos, rot_dim, std::log(theta)));
@@ -565,6 +568,7 @@ ssn_status_t stage_qk_rope_forward(const stage_qk_rope_t *op, const void *q, int
   if (st != SSN_OK) return st;
   if (n_tokens < 0 || n_tokens > (int64_t)1 << 40 || q_heads < 0 || k_heads < 0) return SSN_ERR_SHAPE;
   if (n_tokens == 0 || (q_heads == 0 && k_heads == 0)) return SSN_OK;
+  if (!aligned_to(pos, 4)) return SSN_ERR_SHAPE;
   if (op->rot_dim > 0 && pos == nullptr && seq_len < 1) return SSN_ERR_SHAPE;
   const int32_t d = op->head_dim;
   const size_t item = op->dtype == SSN_F32 ? 4 : 2;
@@ -604,7 +608,7 @@ ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, i
   const size_t item = op->dtype == SSN_F32 ? 4 : 2;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   RopeArgs a{};
-  int launches = 0;
+  if (!aligned_to(pos, 4) || !aligned_to(dwq, 4) || !aligned_to(dwk, 4)) return SSN_ERR_SHAPE;
   if (rows) {
     if (op->rot_dim > 0 && pos == nullptr && seq_len < 1) return SSN_ERR_SHAPE;
     if ((st = check_heads(dq, dq_token, dq_head, n_tokens, q_heads, d, item, false)) != SSN_OK) return st;
@@ -627,7 +631,6 @@ ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, i
     if (dwq != nullptr) a.side[0].partial = partial;
     if (dwk != nullptr) a.side[1].partial = partial + (int64_t)a.side[0].blocks * d;
     if ((st = launch_rope<true>(op, a, v, s)) != SSN_OK) return st;
-    ++launches;
   }
   if (dwq != nullptr || dwk != nullptr) {
     GainArgs g{{a.side[0].partial, a.side[1].partial}, {dwq, dwk}, {a.side[0].blocks, a.side[1].blocks}, d};

@@ -22,3 +22,8 @@ def test_call_values(libssn, change, status):
 
 def test_no_tokens(libssn):
     assert _call(libssn, n=0, logits=None, ids=None, top=None, loss=None, out=None) == libssn.SSN_OK
+
+
+@pytest.mark.parametrize("name", ["ids", "top", "weight", "loss"])
+def test_addresses_off_their_element(libssn, name):
+    assert _call(libssn, **{name: A + 2}) == libssn.SSN_ERR_SHAPE

@@ -33,3 +33,8 @@ def test_empty_calls(libssn):
     assert _quantize(libssn, rows=0, x=None, q=None, scale=None) == libssn.SSN_OK
     assert _matmul(libssn, n=0, xq=None, xs=None, y=None) == libssn.SSN_OK
     assert _matmul(libssn, outer=0, wq=None, ws=None, y=None) == libssn.SSN_OK
+
+
+def test_addresses_off_their_element(libssn):
+    assert _quantize(libssn, scale=A + 2) == libssn.SSN_ERR_SHAPE
+    assert _matmul(libssn, xs=A + 1) == libssn.SSN_ERR_SHAPE and _matmul(libssn, ws=A + 2) == libssn.SSN_ERR_SHAPE

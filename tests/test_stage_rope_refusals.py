@@ -54,3 +54,9 @@ def test_empty_calls_and_workspace(libssn):
     for args in ((A, 64, 16, 63, 1e4), (A, 62, 16, 64, 1e4), (A, 64, -1, 64, 1e4), (A, 64, 16, 64, 0.0), (A, 64, 16, 64, float("inf")), (A, 64, 16, 0, 1e4)):
         assert table(*args, None) == b.SSN_ERR_SHAPE
     assert table(None, 64, 16, 64, 1e4, None) == b.SSN_ERR_NULL and table(None, 64, 0, 64, 1e4, None) == b.SSN_OK
+
+
+@pytest.mark.parametrize("change", [dict(table=A + 2), dict(wq=A + 1), dict(wk=A + 1), dict(dev_status=A + 2)])
+def test_addresses_off_their_element(libssn, change):
+    assert _forward(libssn, _op(libssn, **change)) == libssn.SSN_ERR_SHAPE
+    assert _forward(libssn, _op(libssn), pos=A + 2) == libssn.SSN_ERR_SHAPE
