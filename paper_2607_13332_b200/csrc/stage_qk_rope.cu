@@ -427,6 +427,11 @@ ssn_status_t check_heads(const void *x, int64_t token, int64_t head, int64_t n, 
   return aligned_to(x, item) ? SSN_OK : SSN_ERR_SHAPE;
 }
 
+// An output that starts where an input starts is that input: with other strides its rows would overwrite rows not read yet
+bool other_strides(const void *out, int64_t out_token, int64_t out_head, const void *x, int64_t token, int64_t head, int64_t n, int32_t heads) {
+  return heads > 0 && out == x && ((n > 1 && out_token != token) || (heads > 1 && out_head != head));
+}
+
 // Elements per piece (a power of two, 16 bytes at most) that every address and stride allows
 struct Width {
   int v;
@@ -576,6 +581,9 @@ ssn_status_t stage_qk_rope_forward(const stage_qk_rope_t *op, const void *q, int
   if ((st = check_heads(k, k_token, k_head, n_tokens, k_heads, d, item, false)) != SSN_OK) return st;
   if ((st = check_heads(q_out, qo_token, qo_head, n_tokens, q_heads, d, item, true)) != SSN_OK) return st;
   if ((st = check_heads(k_out, ko_token, ko_head, n_tokens, k_heads, d, item, true)) != SSN_OK) return st;
+  if (other_strides(q_out, qo_token, qo_head, q, q_token, q_head, n_tokens, q_heads) ||
+      other_strides(k_out, ko_token, ko_head, k, k_token, k_head, n_tokens, k_heads))
+    return SSN_ERR_SHAPE;
   RopeArgs a{};
   fill(op, a, pos, n_tokens, seq_len);
   const RopeSide qs{q, nullptr, q_out, op->wq, nullptr, q_token, q_head, 0, 0, qo_token, qo_head, q_heads, 0, 1, 1};
@@ -617,6 +625,11 @@ ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, i
     if ((st = check_heads(k, k_token, k_head, n_tokens, k_heads, d, item, false)) != SSN_OK) return st;
     if ((st = check_heads(dq_in, dqi_token, dqi_head, n_tokens, q_heads, d, item, true)) != SSN_OK) return st;
     if ((st = check_heads(dk_in, dki_token, dki_head, n_tokens, k_heads, d, item, true)) != SSN_OK) return st;
+    if (other_strides(dq_in, dqi_token, dqi_head, dq, dq_token, dq_head, n_tokens, q_heads) ||
+        other_strides(dk_in, dki_token, dki_head, dk, dk_token, dk_head, n_tokens, k_heads) ||
+        other_strides(dq_in, dqi_token, dqi_head, q, q_token, q_head, n_tokens, q_heads) ||
+        other_strides(dk_in, dki_token, dki_head, k, k_token, k_head, n_tokens, k_heads))
+      return SSN_ERR_SHAPE;
     if ((dwq != nullptr || dwk != nullptr) &&
         (workspace == nullptr || !aligned_to(workspace, 16) || workspace_bytes < stage_qk_rope_workspace_bytes(op, n_tokens, q_heads, k_heads)))
       return SSN_ERR_WORKSPACE;

@@ -9,7 +9,7 @@ from typing import Optional, Tuple
 import torch
 
 from . import binding
-from .runner import _TORCH_DTYPE, _ld, _ptr, _stream
+from .runner import _TORCH_DTYPE, _ptr, _stream
 
 _lib = binding.library()
 _CODES = {torch.float32: binding.SSN_F32, torch.bfloat16: binding.SSN_BF16}
@@ -33,9 +33,9 @@ def _here(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:
 def _pitch(t: torch.Tensor, rows: int, cols: int) -> int:
     """Leading dimension of a row-major [rows, cols] tensor, in elements."""
     ld, unit = t.stride()
-    if unit != 1 and cols > 1:
+    if (unit != 1 and cols > 1) or (rows > 1 and ld < cols):     # rows that share elements have no leading dimension
         raise ValueError("expected a row-major 2-D tensor (unit stride along the last dimension)")
-    return ld if rows > 1 and ld > cols else cols
+    return ld if rows > 1 else cols
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) -> int:
@@ -70,8 +70,9 @@ class QKNormRope:
         if table is not None:
             max_pos, rot = _here(table, torch.float32, "table").shape
         self.dev_status = torch.zeros(1, dtype=torch.int32, device=device)
+        self._device = _here(self.dev_status, torch.int32, "device").get_device()     # calls are for this device alone
         self.c = binding.make_qk_rope(head_dim, rot, binding.DTYPES[dtype], binding.PAIRINGS[pairing], eps, _ptr(wq), _ptr(wk),
-                                      _ptr(table), _ld(table) if table is not None else 0, max_pos, self.dev_status.data_ptr())
+                                      _ptr(table), _pitch(table, max_pos, rot) if table is not None else 0, max_pos, self.dev_status.data_ptr())
         self._ref = byref(self.c)
         self._workspace = {}
 
@@ -87,8 +88,8 @@ class QKNormRope:
             if n * heads:
                 raise ValueError(f"{what} is missing")
             return 0, 0, 0
-        if t.dtype != self.dtype or t.get_device() != _current_device():
-            raise ValueError(f"{what}: expected {self.dtype} on the current device")
+        if t.dtype != self.dtype or t.get_device() != self._device:
+            raise ValueError(f"{what}: expected {self.dtype} on the operator's device")
         if t.shape != (n, heads, self.head_dim):
             raise ValueError(f"{what}: expected [{n}, {heads}, {self.head_dim}]")
         token, head, unit = t.stride()
@@ -106,13 +107,14 @@ class QKNormRope:
         t = _new((n, heads, d), (heads * d, d, 1), self.dtype)
         return t, (t.data_ptr(), heads * d, d)
 
-    @staticmethod
-    def _sizes(q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> Tuple[int, int, int]:
+    def _sizes(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> Tuple[int, int, int]:
         some = q if q is not None else k
         if some is None:
             raise ValueError("neither queries nor keys")
         if some.dim() != 3:
             raise ValueError("expected [tokens, heads, head_dim]")
+        if _current_device() != self._device:     # its stream is the one that the kernel is put on
+            raise ValueError("the current device is not the operator's")
         return some.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
 
     def forward(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Optional[torch.Tensor] = None, seq_len: int = 0,

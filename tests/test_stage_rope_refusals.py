@@ -3,6 +3,7 @@
 import ctypes
 
 import pytest
+import torch
 
 A = 0x10000      # an aligned address that no call here reaches
 
@@ -60,3 +61,45 @@ def test_empty_calls_and_workspace(libssn):
 def test_addresses_off_their_element(libssn, change):
     assert _forward(libssn, _op(libssn, **change)) == libssn.SSN_ERR_SHAPE
     assert _forward(libssn, _op(libssn), pos=A + 2) == libssn.SSN_ERR_SHAPE
+
+
+def test_an_output_in_place_of_an_input_of_other_strides(libssn):
+    b = libssn
+    other = dict(q=(2 * A, 256, 64), k=(3 * A, 64, 64), qo=(4 * A, 256, 64), ko=(5 * A, 64, 64))
+    assert _forward(b, _op(b), **dict(other, q=(A, 320, 64), qo=(A, 256, 64))) == b.SSN_ERR_SHAPE
+    assert _forward(b, _op(b), **dict(other, k=(A, 64, 64), ko=(A, 128, 64))) == b.SSN_ERR_SHAPE
+    back = b.raw("stage_qk_rope_backward")
+    for out in ((A, 128, 64), (2 * A, 128, 64)):      # dq and q start there
+        assert back(ctypes.byref(_op(b)), A, 64, 64, 3 * A, 64, 64, 2 * A, 64, 64, 1, 4 * A, 64, 64, 1, *out, 5 * A, 64, 64, None, None,
+                    None, 3, 8, None, 0, None) == b.SSN_ERR_SHAPE
+
+
+@pytest.fixture
+def host_is_current(monkeypatch):
+    """Tensors on the host pass for tensors of the current device: no call below reaches the library."""
+    stage_ops = pytest.importorskip("paper_2607_13332_b200.stage_ops")
+    monkeypatch.setattr(stage_ops, "_current_device", lambda: -1)
+    return stage_ops
+
+
+def test_rows_that_share_elements_have_no_leading_dimension(libssn, host_is_current):
+    row = torch.zeros(1, 8)
+    assert host_is_current._pitch(row.expand(1, 8), 1, 8) == 8
+    assert host_is_current._pitch(torch.zeros(3, 10)[:, :8], 3, 8) == 10
+    for shared in (row.expand(4, 8), torch.zeros(64).as_strided((4, 8), (7, 1)), torch.zeros(4, 16)[:, ::2]):
+        with pytest.raises(ValueError, match="row-major"):
+            host_is_current._pitch(shared, 4, 8)
+    with pytest.raises(ValueError, match="row-major"):
+        host_is_current.QKNormRope("f32", 8, table=row.expand(4, 8), device="cpu")
+
+
+def test_an_operator_is_for_one_device(libssn, host_is_current, monkeypatch):
+    op = host_is_current.QKNormRope("f32", 8, device="cpu")
+    q = torch.zeros(2, 1, 8)
+    monkeypatch.setattr(host_is_current, "_current_device", lambda: 1)
+    with pytest.raises(ValueError, match="device"):
+        op.forward(q, None, seq_len=2)
+    with pytest.raises(ValueError, match="device"):
+        op.backward(q, None, q, None, seq_len=2)
+    with pytest.raises(ValueError, match="device"):      # its status word would lie elsewhere
+        host_is_current.QKNormRope("f32", 8, device="cpu")
