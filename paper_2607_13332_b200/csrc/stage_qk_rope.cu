@@ -264,7 +264,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
       v_fma(sq, xa[n], xa[n], sq);
       v_fma(sq, xb[n], xb[n], sq);
     }
-    const float r = rsqrtf(fmaf(group_sum(v_total(sq), lg), inv_d, a.eps));
+    float r = rsqrtf(fmaf(group_sum(v_total(sq), lg), inv_d, a.eps));
+    if (BACK && !there) r = 0.f;   // a row that is not there: with eps = 0 its zeros would be NaN in the gains' sums
     if (!BACK) {
 #pragma unroll
       for (int n = 0; n < NU; ++n) {

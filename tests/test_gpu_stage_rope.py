@@ -62,7 +62,7 @@ def pair_bound(x, rot, pairing):
 
 def check(got, want, bound, dt, what):
     limit = torch.finfo(dt).eps / 2 * np.abs(want) * (1 + 1e-6) + bound + 1e-37
-    bad = np.abs(f64(got) - want) > limit
+    bad = ~(np.abs(f64(got) - want) <= limit)      # a NaN is off
     assert not bad.any(), f"{what}: {bad.sum()} values off, worst {np.max(np.abs(f64(got) - want) / limit):.2f} of the limit"
 
 
@@ -143,6 +143,20 @@ def test_backward(case):
         # at most 100 rows per lane one after the other, 13 steps over lanes and warps, then 64 bits
         check(got[2 + i], dw, 150 * U * (g * u).sum(axis=(0, 1)), torch.float32, "gain")
         assert untouched(out, buf) and torch.equal(again[i], out) and torch.equal(again[2 + i], got[2 + i])
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("bf16", 20)])
+def test_gains_without_eps(dtype, d):
+    """eps = 0: lanes without a head add nothing, although the root of their zeros is infinite."""
+    rng, dt = np.random.default_rng(d), TORCH[dtype]
+    q, k, dq, dk = (heads(rng, 7, h, d, dt, "plain")[0] for h in (5, 1, 5, 1))
+    got = QKNormRope(dtype, d, eps=0.0).backward(dq, dk, q, k)
+    for x, dy, dx, dw in zip((q, k), (dq, dk), got[:2], got[2:]):
+        want_x, want_w = so.qk_rope_backward(f64(dy), f64(x), None, np.zeros((7, 0)), "halves", 0.0)
+        r = so.qk_norm(f64(x), None, 0.0)[1]
+        u, g = np.abs(f64(x)) * r, np.abs(f64(dy))
+        check(dx, want_x, 40 * U * r * (g + u * (g * u).mean(axis=-1, keepdims=True)), dt, "backward")
+        check(dw, want_w, 150 * U * (g * u).sum(axis=(0, 1)), torch.float32, "gain")
 
 
 def test_in_place_and_without_gains():
