@@ -1,12 +1,11 @@
 // Query/key norm with rotary positions (include/agora_stage.h), forward and backward.
 //
 // A row is one head of one token: D values, one mean of squares, one pass.  Both directions move two (three) rows of D per
-// row and compute a few operations per value: HBM bounds the forward pass (65536 tokens x 40 heads of 128 bf16 in 224 us,
-// 6.0 TB/s, 0.92 of a copy), the instructions the gradients (32768 tokens in 215 us, 4.7 TB/s: 426 per warp and four rows, two
-// of three issue slots).
+// row and compute a few operations per value: HBM bounds the forward pass (65536 tokens x 40 heads of 128 bf16 in 217 us,
+// 6.2 TB/s, 0.95 of a copy), HBM and instruction issue the gradients (32768 tokens in 179 us, 5.6 TB/s, 0.86).
 //
 // A row belongs to a group of G lanes (a power of two).  A lane's unit is V column PAIRS, so that no shuffle moves values:
-// for halves one 16-byte piece at column i and one at i + rot_dim / 2, for adjacent pairs two pieces in a row.  The columns
+// for halves one 16-byte piece at column i and one at i + rot_dim / 2, for adjacent pairs at i and i + D / 2.  The columns
 // past rot_dim are paired in the same way (i with i + (D - rot_dim) / 2) and pass the rotation untouched.  A warp keeps the
 // table row of its token in registers and goes through the token's heads, 32 / G at a time; blocks are dealt to the query
 // and the key side by their numbers of heads, so that a warp needs one gain (and one gradient of it) only.  Rows are loaded
@@ -19,10 +18,10 @@ namespace ssn {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-// Resident blocks, and passes of rows on their way per warp.  65536 x 40 heads of 128 bf16 forward: two blocks four or six passes
-// ahead 224 us, three blocks spill (365).  The gradients of 32768: two to four passes ahead 211-216 us.
+// Resident blocks, and passes of rows on their way per warp.  65536 x 40 heads of 128 bf16 forward: two blocks three passes ahead
+// 217 us, two 234, four or six 248, three blocks spill (336).  The gradients of 32768: two passes ahead 183 us, three or four 179.
 constexpr int kPerSm = 2;
-constexpr int kForwardAhead = 4, kBackAhead = 3;
+constexpr int kForwardAhead = 3, kBackAhead = 3;
 
 struct RopeSide {
   const void *x, *dy;   // forward input; incoming gradient (backward)
@@ -55,9 +54,12 @@ __device__ __forceinline__ int32_t table_row(const RopeArgs &a, int64_t t) {
   return -1;
 }
 
-// V column pairs (a, b) in two pieces of V elements: the halves' pieces are the a and the b, adjacent pairs alternate
+// V column pairs (a, b) in two pieces of V elements: the halves' pieces are the a and the b; of adjacent pairs either piece holds
+// V / 2, or its half of the only one
 template <typename T, int V, bool ADJ> struct Unit {
   Chunk<T, V> p0, p1;
+  static __device__ __forceinline__ int a_column(int at0, int at1, int i) { return !ADJ || V == 1 ? at0 + i : 2 * i < V ? at0 + 2 * i : at1 + 2 * i - V; }
+  static __device__ __forceinline__ int b_column(int at0, int at1, int i) { return !ADJ || V == 1 ? at1 + i : a_column(at0, at1, i) + 1; }
   __device__ __forceinline__ void load(const T *x, int at0, int at1) {
     p0.load(x + at0);
     p1.load(x + at1);
@@ -93,11 +95,15 @@ template <typename T, int V, bool ADJ> struct Unit {
 };
 
 // Copies a piece to shared memory behind this thread's back; two bytes are more than cp.async can (they wait here)
-template <int BYTES> __device__ __forceinline__ void copy_piece(unsigned char *to, const void *from, bool there = true) {
-  const uint32_t at = smem_address(to), bytes = there ? BYTES : 0;   // the rest becomes zeros
-  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(at), "l"(from), "r"(bytes) : "memory");
-  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;\n" ::"r"(at), "l"(from), "n"(BYTES), "r"(bytes) : "memory");
-  else *reinterpret_cast<uint16_t *>(to) = there ? *static_cast<const uint16_t *>(from) : (uint16_t)0;
+template <int BYTES> __device__ __forceinline__ void copy_piece(unsigned char *to, const void *from) {
+  const uint32_t at = smem_address(to);
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(at), "l"(from) : "memory");
+  else if constexpr (BYTES >= 4) asm volatile("cp.async.ca.shared.global [%0], [%1], %2;\n" ::"r"(at), "l"(from), "n"(BYTES) : "memory");
+  else *reinterpret_cast<uint16_t *>(to) = *static_cast<const uint16_t *>(from);
+}
+template <int BYTES> __device__ __forceinline__ void clear_piece(unsigned char *to) {
+  RawBytes<BYTES> zero = {};
+  *reinterpret_cast<RawBytes<BYTES> *>(to) = zero;
 }
 
 __device__ __forceinline__ float group_sum(float x, int group_log2) {
@@ -118,10 +124,11 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
   __shared__ float sums[BACK ? kWarps : 1][BACK ? STAGE_MAX_HEAD_DIM : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int side = (int)blockIdx.x >= a.side[0].blocks ? 1 : 0;
-  const RopeSide &s = a.side[side];
+  const RopeSide s = side ? a.side[1] : a.side[0];
   const int block = (int)blockIdx.x - (side ? a.side[0].blocks : 0);
   const int lg = a.group_log2, rows_per_pass = 32 >> lg, row = lane >> lg, unit0 = lane & ((1 << lg) - 1);
   const int half = a.rot >> 1, rest = (a.d - a.rot) >> 1;
+  constexpr bool kSpread = ADJ && V > 1;   // a unit's pieces lie half a row apart, so that lanes side by side take bytes side by side
   unsigned char *ring = dyn + warp * (P * kPassBytes + kTables * a.table_bytes);
   float *tables = reinterpret_cast<float *>(ring + P * kPassBytes);
   const int table_floats = a.table_bytes / 4;
@@ -134,10 +141,13 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
   for (int n = 0; n < NU; ++n) {
     pair[n] = (unit0 + (n << lg)) * V;
     mine[n] = FULL || 2 * pair[n] < a.d;
-    turned[n] = FULL || pair[n] < half;   // FULL: every column turns
-    if (ADJ) {
+    turned[n] = FULL || (kSpread ? half > 0 && mine[n] : pair[n] < half);   // FULL: every column turns
+    if (kSpread) {
+      at0[n] = pair[n];
+      at1[n] = at0[n] + (a.d >> 1);
+    } else if (ADJ) {
       at0[n] = 2 * pair[n];
-      at1[n] = at0[n] + V;
+      at1[n] = at0[n] + 1;
     } else {
       at0[n] = turned[n] ? pair[n] : a.rot + pair[n] - half;
       at1[n] = at0[n] + (turned[n] ? half : rest);
@@ -166,22 +176,23 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
   const int64_t t0 = wid / s.parts;
   const int64_t steps = wid < slots * s.parts && t0 < a.n ? (a.n - t0 + slots - 1) / slots * passes : 0;   // passes over all its tokens
   // a pointer goes from pass to pass, and from a token's last pass to the next token's first
-  const T *x = static_cast<const T *>(s.x) + t0 * s.x_token + (first + row) * s.x_head;
-  const T *dy = BACK ? static_cast<const T *>(s.dy) + t0 * s.dy_token + (first + row) * s.dy_head : nullptr;
-  T *out = static_cast<T *>(s.out) + t0 * s.out_token + (first + row) * s.out_head;
+  // (at the lane's first piece)
+  const T *x = static_cast<const T *>(s.x) + t0 * s.x_token + (first + row) * s.x_head + at0[0];
+  const T *dy = BACK ? static_cast<const T *>(s.dy) + t0 * s.dy_token + (first + row) * s.dy_head + at0[0] : nullptr;
+  T *out = static_cast<T *>(s.out) + t0 * s.out_token + (first + row) * s.out_head + at0[0];
   const int64_t x_step = rows_per_pass * s.x_head, dy_step = rows_per_pass * s.dy_head, out_step = rows_per_pass * s.out_head;
   const int64_t x_jump = slots * s.x_token - passes * x_step, dy_jump = slots * s.dy_token - passes * dy_step;
   const int64_t out_jump = slots * s.out_token - passes * out_step;
 
   // the copies, P passes ahead of the rows in hand
   int64_t ahead_t = t0, ahead_left = steps;
-  int ahead_row = row, ahead_table = 0;
+  int ahead_head = 0, ahead_table = 0;   // the pass's first head
   uint32_t ahead_place = 0;
   int32_t ahead_pos = a.rot > 0 && steps > 0 ? table_row(a, t0) : 0;
   auto copy_pass = [&]() {
     if (ahead_left > 0) {
       --ahead_left;
-      if (ahead_row == row && a.rot > 0) {
+      if (ahead_head == 0 && (FULL || a.rot > 0)) {
         float *to = tables + ahead_table * table_floats;
         const float *from = a.table + ahead_pos * a.ldt;
         if (ahead_pos < 0)
@@ -198,20 +209,27 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
       unsigned char *to = ring + ahead_place + lane * kPieceBytes;
 #pragma unroll
       for (int n = 0; n < NU; ++n) {
-        const bool there = mine[n] && ahead_row < heads;
-        const T *from = there ? x : static_cast<const T *>(s.x), *from_dy = BACK ? there ? dy : static_cast<const T *>(s.dy) : nullptr;
-        copy_piece<kPieceBytes>(to + n * kUnitBytes, from + (there ? at0[n] : 0), there);
-        copy_piece<kPieceBytes>(to + n * kUnitBytes + 32 * kPieceBytes, from + (there ? at1[n] : 0), there);
-        if (BACK) {
-          copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes, from_dy + (there ? at0[n] : 0), there);
-          copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes + 32 * kPieceBytes, from_dy + (there ? at1[n] : 0), there);
+        if (mine[n] && ahead_head + row < heads) {
+          const int o0 = at0[n] - at0[0], o1 = at1[n] - at0[0];
+          copy_piece<kPieceBytes>(to + n * kUnitBytes, x + o0);
+          copy_piece<kPieceBytes>(to + n * kUnitBytes + 32 * kPieceBytes, x + o1);
+          if (BACK) {
+            copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes, dy + o0);
+            copy_piece<kPieceBytes>(to + (NU + n) * kUnitBytes + 32 * kPieceBytes, dy + o1);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < (BACK ? 2 : 1); ++i) {
+            clear_piece<kPieceBytes>(to + (i * NU + n) * kUnitBytes);
+            clear_piece<kPieceBytes>(to + (i * NU + n) * kUnitBytes + 32 * kPieceBytes);
+          }
         }
       }
-      ahead_row += rows_per_pass;
+      ahead_head += rows_per_pass;
       x += x_step;
       if (BACK) dy += dy_step;
-      if (ahead_row - row >= heads) {
-        ahead_row = row;
+      if (ahead_head >= heads) {
+        ahead_head = 0;
         x += x_jump;
         if (BACK) dy += dy_jump;
       }
@@ -226,20 +244,25 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
   // forward: y_a = r (x_a (w_a cos) - x_b (w_b sin)), y_b = r (x_b (w_b cos) + x_a (w_a sin)); the products of the gain and the
   // angle serve all heads of the token.  backward: cosine, sine, minus sine.
   float ca[NU][V], cb[BACK ? 1 : NU][V], sa[NU][V], sb[NU][V];
-  int now = row, table = 0;   // the lane's row among the part's heads
+  int now = 0, table = 0;   // the pass's first head
   uint32_t place_at = 0;
 #pragma unroll 1
   for (int64_t left = steps; left > 0; --left) {
     asm volatile("cp.async.wait_group %0;\n" ::"n"(P - 1) : "memory");
     __syncwarp();
-    if (now == row) {   // a token's first pass
+    if (now == 0) {   // a token's first pass
       const float *cs = tables + table * table_floats;
 #pragma unroll
       for (int n = 0; n < NU; ++n)
         if (turned[n] && (FULL ? NU == 1 || mine[n] : mine[n])) {
           float c[V], sn[V];
 #pragma unroll
-          for (int i = 0; i < V; ++i) c[i] = cs[pair[n] + i], sn[i] = cs[half + pair[n] + i];
+          for (int i = 0; i < V; ++i) {
+            const int p = kSpread ? Unit<T, V, ADJ>::a_column(at0[n], at1[n], i) >> 1 : pair[n] + i;
+            const bool turns = FULL || !kSpread || p < half;
+            c[i] = turns ? cs[p] : 1.f;
+            sn[i] = turns ? cs[half + p] : 0.f;
+          }
           if (BACK) {
 #pragma unroll
             for (int i = 0; i < V; ++i) ca[n][i] = c[i], sa[n][i] = sn[i], sb[n][i] = -sn[i];
@@ -253,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
         }
       if (++table == kTables) table = 0;
     }
-    const bool there = now < heads;
+    const bool there = now + row < heads;
     const unsigned char *place = ring + place_at + lane * kPieceBytes;
     float xa[NU][V], xb[NU][V], oa[NU][V], ob[NU][V], sq[V] = {};
 #pragma unroll
@@ -282,7 +305,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
         }
       }
     } else {
-      // g: the gradient turned back; sums of g x w for the row and of g x r for the gain
+      // g: the gradient turned back, times r; sums of g x w for the row and of g x for the gain
       float in[V] = {};
 #pragma unroll
       for (int n = 0; n < NU; ++n) {
@@ -299,19 +322,16 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
 #pragma unroll
           for (int i = 0; i < V; ++i) ga[i] = ta[i];
         }
-        float q[V];
-        v_mul(q, ga, xa[n]);
-        v_axpy(dwa[n], r, q, dwa[n]);
-        v_fma(in, q, wa[n], in);
-        v_mul(q, gb, xb[n]);
-        v_axpy(dwb[n], r, q, dwb[n]);
-        v_fma(in, q, wb[n], in);
-        v_mul(ga, ga, wa[n]);
-        v_mul(gb, gb, wb[n]);
-        v_scale(oa[n], r, ga);
-        v_scale(ob[n], r, gb);
+        v_scale(ga, r, ga);
+        v_scale(gb, r, gb);
+        v_fma(dwa[n], ga, xa[n], dwa[n]);
+        v_fma(dwb[n], gb, xb[n], dwb[n]);
+        v_mul(oa[n], ga, wa[n]);
+        v_mul(ob[n], gb, wb[n]);
+        v_fma(in, oa[n], xa[n], in);
+        v_fma(in, ob[n], xb[n], in);
       }
-      const float k = -(r * (r * (r * (group_sum(v_total(in), lg) * inv_d))));   // dx = r (g w - x r^2 mean(g w x))
+      const float k = -(r * (r * (group_sum(v_total(in), lg) * inv_d)));   // dx = r g w - x r^2 mean(r g w x)
 #pragma unroll
       for (int n = 0; n < NU; ++n) {
         v_axpy(oa[n], k, xa[n], oa[n]);
@@ -323,12 +343,12 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
       if (mine[n] && there) {
         Unit<T, V, ADJ> o;
         o.pack(oa[n], ob[n]);
-        o.store(out, at0[n], at1[n]);
+        o.store(out, at0[n] - at0[0], at1[n] - at0[0]);
       }
     out += out_step;
     now += rows_per_pass;
-    if (now - row >= heads) {
-      now = row;
+    if (now >= heads) {
+      now = 0;
       out += out_jump;
     }
     place_at += kPassBytes;
@@ -347,8 +367,8 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
           dwb[n][i] += __shfl_xor_sync(0xffffffffu, dwb[n][i], o);
         }
         if (row == 0 && mine[n]) {
-          sums[warp][at0[n] + (ADJ ? 2 * i : i)] = dwa[n][i];
-          sums[warp][ADJ ? at0[n] + 2 * i + 1 : at1[n] + i] = dwb[n][i];
+          sums[warp][Unit<T, V, ADJ>::a_column(at0[n], at1[n], i)] = dwa[n][i];
+          sums[warp][Unit<T, V, ADJ>::b_column(at0[n], at1[n], i)] = dwb[n][i];
         }
       }
     __syncthreads();
@@ -532,8 +552,12 @@ void fill(const stage_qk_rope_t *op, RopeArgs &a, const int32_t *pos, int64_t n,
 int width_of(const stage_qk_rope_t *op, const RopeArgs &a, bool back) {
   const size_t item = op->dtype == SSN_F32 ? 4 : 2;
   Width w(item);
-  w.stride(a.rot / 2);
-  w.stride((a.d - a.rot) / 2);
+  if (op->pairing == STAGE_PAIR_ADJACENT) {
+    w.stride(a.d / 2);
+  } else {
+    w.stride(a.rot / 2);
+    w.stride((a.d - a.rot) / 2);
+  }
   for (const RopeSide &s : a.side) {
     if (s.heads == 0) continue;
     w.address(s.x, item);
