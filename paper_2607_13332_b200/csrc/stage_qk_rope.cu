@@ -5,8 +5,8 @@
 // 6.2 TB/s, 0.95 of a copy), HBM and instruction issue the gradients (32768 tokens in 179 us, 5.6 TB/s, 0.86).
 //
 // A row belongs to a group of G lanes (a power of two).  A lane's unit is V column PAIRS, so that no shuffle moves values:
-// for halves one 16-byte piece at column i and one at i + rot_dim / 2, for adjacent pairs at i and i + D / 2.  The columns
-// past rot_dim are paired in the same way (i with i + (D - rot_dim) / 2) and pass the rotation untouched.  A warp keeps the
+// for halves one 16-byte piece at column i and one at i + rot_dim / 2, for adjacent pairs at i and i + D / 2.  The halves'
+// columns past rot_dim are paired in the same way (i with i + (D - rot_dim) / 2) and pass the rotation untouched.  A warp keeps the
 // table row of its token in registers and goes through the token's heads, 32 / G at a time; blocks are dealt to the query
 // and the key side by their numbers of heads, so that a warp needs one gain (and one gradient of it) only.  Rows are loaded
 // through a ring in shared memory: loads into registers, as many as fit, left the forward pass at 259 us.
@@ -113,22 +113,29 @@ __device__ __forceinline__ float group_sum(float x, int group_log2) {
   return x;
 }
 
+// How pairs of columns come together: both in a lane's unit (HALVES, ADJACENT), or, for halves whose distance is no multiple of V,
+// from the row in shared memory (CROSSED): a lane turns the columns of its two pieces and reads their partners one by one.
+enum Pairs { HALVES, ADJACENT, CROSSED };
+
 // NU units per lane (more than one only where V is small).  A warp's rows come through a ring in shared memory: every lane
 // copies its own pieces kAhead passes ahead (cp.async, no registers held), and the warp together the table rows of the tokens
 // that these passes begin.
-template <typename T, int V, int NU, bool ADJ, bool BACK, bool FULL>
+template <typename T, int V, int NU, Pairs PAIRS, bool BACK, bool FULL>
 __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int P = BACK ? kBackAhead : kForwardAhead, kPieceBytes = V * (int)sizeof(T), kUnitBytes = 2 * 32 * kPieceBytes;
   constexpr int kPassBytes = (BACK ? 2 : 1) * NU * kUnitBytes, kTables = P + 1;
   extern __shared__ __align__(16) unsigned char dyn[];
   __shared__ float sums[BACK ? kWarps : 1][BACK ? STAGE_MAX_HEAD_DIM : 1];
+  __shared__ __align__(16) float gains[PAIRS == CROSSED ? STAGE_MAX_HEAD_DIM : 1];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int side = (int)blockIdx.x >= a.side[0].blocks ? 1 : 0;
   const RopeSide s = side ? a.side[1] : a.side[0];
   const int block = (int)blockIdx.x - (side ? a.side[0].blocks : 0);
   const int lg = a.group_log2, rows_per_pass = 32 >> lg, row = lane >> lg, unit0 = lane & ((1 << lg) - 1);
   const int half = a.rot >> 1, rest = (a.d - a.rot) >> 1;
-  constexpr bool kSpread = ADJ && V > 1;   // a unit's pieces lie half a row apart, so that lanes side by side take bytes side by side
+  constexpr bool ADJ = PAIRS == ADJACENT, kCrossed = PAIRS == CROSSED;
+  static_assert(!kCrossed || (NU == 1 && !FULL), "one unit per lane");
+  constexpr bool kSpread = (ADJ && V > 1) || kCrossed;   // a unit's pieces lie half a row apart, so that lanes side by side take bytes side by side
   unsigned char *ring = dyn + warp * (P * kPassBytes + kTables * a.table_bytes);
   float *tables = reinterpret_cast<float *>(ring + P * kPassBytes);
   const int table_floats = a.table_bytes / 4;
@@ -152,7 +159,7 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
       at0[n] = turned[n] ? pair[n] : a.rot + pair[n] - half;
       at1[n] = at0[n] + (turned[n] ? half : rest);
     }
-    if (mine[n] && s.w != nullptr) {
+    if (!kCrossed && mine[n] && s.w != nullptr) {
       Unit<T, V, ADJ> w;
       w.load(static_cast<const T *>(s.w), at0[n], at1[n]);
       w.get(wa[n], wb[n]);
@@ -161,6 +168,25 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
       for (int i = 0; i < V; ++i) wa[n][i] = wb[n][i] = 1.f;
     }
   }
+  uint32_t partner_at[V];   // where the columns' partners lie among the pieces of a pass, in bytes: 16 bits each
+  auto partner = [&](int c) { return c < half ? c + half : c < a.rot ? c - half : c; };
+  if (kCrossed) {
+    for (int c = threadIdx.x; c < a.d; c += kThreads) gains[c] = s.w != nullptr ? to_f32<T>(static_cast<const T *>(s.w)[c]) : 1.f;
+    __syncthreads();
+    auto place_of = [&](int c) {
+      c = mine[0] ? partner(c) : 0;
+      return (row << lg) * kPieceBytes + (c < (a.d >> 1) ? c * (int)sizeof(T) : 32 * kPieceBytes + (c - (a.d >> 1)) * (int)sizeof(T));
+    };
+#pragma unroll
+    for (int i = 0; i < V; ++i) partner_at[i] = (uint32_t)place_of(at0[0] + i) | (uint32_t)place_of(at1[0] + i) << 16;
+  }
+  auto partners = [&](const unsigned char *place, float (&pa)[V], float (&pb)[V]) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      pa[i] = to_f32<T>(*reinterpret_cast<const T *>(place + (partner_at[i] & 0xffff)));
+      pb[i] = to_f32<T>(*reinterpret_cast<const T *>(place + (partner_at[i] >> 16)));
+    }
+  };
   float dwa[NU][V], dwb[NU][V];
 #pragma unroll
   for (int n = 0; n < NU; ++n)
@@ -242,8 +268,12 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
   for (int i = 0; i < P; ++i) copy_pass();
 
   // forward: y_a = r (x_a (w_a cos) - x_b (w_b sin)), y_b = r (x_b (w_b cos) + x_a (w_a sin)); the products of the gain and the
-  // angle serve all heads of the token.  backward: cosine, sine, minus sine.
+  // angle serve all heads of the token.  backward: cosine, sine, minus sine.  CROSSED: the factors of a column and of its partner
   float ca[NU][V], cb[BACK ? 1 : NU][V], sa[NU][V], sb[NU][V];
+  if (kCrossed) {   // lanes without columns
+#pragma unroll
+    for (int i = 0; i < V; ++i) ca[0][i] = cb[0][i] = sa[0][i] = sb[0][i] = 0.f;
+  }
   int now = 0, table = 0;   // the pass's first head
   uint32_t place_at = 0;
 #pragma unroll 1
@@ -252,9 +282,22 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
     __syncwarp();
     if (now == 0) {   // a token's first pass
       const float *cs = tables + table * table_floats;
+      if (kCrossed) {
+        auto factors = [&](int c, float &own, float &other) {
+          const int p = c < half ? c : c - half;
+          own = c < a.rot ? cs[p] : 1.f;
+          other = c < a.rot ? cs[half + p] : 0.f;
+          if ((c < half) != BACK) other = -other;
+          if (!BACK) own *= gains[c], other *= gains[partner(c)];
+        };
+        if (mine[0]) {
+#pragma unroll
+          for (int i = 0; i < V; ++i) factors(at0[0] + i, ca[0][i], sa[0][i]), factors(at1[0] + i, cb[0][i], sb[0][i]);
+        }
+      }
 #pragma unroll
       for (int n = 0; n < NU; ++n)
-        if (turned[n] && (FULL ? NU == 1 || mine[n] : mine[n])) {
+        if (!kCrossed && turned[n] && (FULL ? NU == 1 || mine[n] : mine[n])) {
           float c[V], sn[V];
 #pragma unroll
           for (int i = 0; i < V; ++i) {
@@ -294,7 +337,16 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
       for (int n = 0; n < NU; ++n) {
         v_scale(xa[n], r, xa[n]);
         v_scale(xb[n], r, xb[n]);
-        if (turned[n]) {
+        if (kCrossed) {
+          float pa[V], pb[V];
+          partners(ring + place_at, pa, pb);
+          v_scale(pa, r, pa);
+          v_scale(pb, r, pb);
+          v_mul(oa[n], xa[n], ca[n]);
+          v_fma(oa[n], pa, sa[n], oa[n]);
+          v_mul(ob[n], xb[n], cb[BACK ? 0 : n]);
+          v_fma(ob[n], pb, sb[n], ob[n]);
+        } else if (turned[n]) {
           v_mul(oa[n], xa[n], ca[n]);
           v_fma(oa[n], xb[n], sb[n], oa[n]);
           v_mul(ob[n], xb[n], cb[BACK ? 0 : n]);
@@ -313,7 +365,18 @@ __global__ void __launch_bounds__(kThreads, kPerSm) qk_rope_kernel(const __grid_
         u.take(place + (NU + n) * kUnitBytes);
         float ga[V], gb[V];
         u.get(ga, gb);
-        if (turned[n]) {
+        if (kCrossed) {
+          float pa[V], pb[V];
+          partners(ring + place_at + kUnitBytes, pa, pb);
+          v_mul(ga, ga, ca[n]);
+          v_fma(ga, pa, sa[n], ga);
+          v_mul(gb, gb, cb[0]);
+          v_fma(gb, pb, sb[n], gb);
+          if (mine[n]) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) wa[n][i] = gains[at0[n] + i], wb[n][i] = gains[at1[n] + i];
+          }
+        } else if (turned[n]) {
           float ta[V];
           v_mul(ta, ga, ca[n]);
           v_fma(ta, gb, sa[n], ta);
@@ -488,39 +551,28 @@ int side_blocks(int sms, int per_sm, int32_t heads, int32_t other, int rows_per_
   return b < 1 ? 1 : (int)b;
 }
 
-template <typename T, int V, int NU, bool ADJ, bool BACK, bool FULL = false>
+template <typename T, int V, int NU, Pairs PAIRS, bool BACK, bool FULL = false>
 cudaError_t launch_unit(const RopeArgs &a, cudaStream_t stream) {
   static std::atomic<uint64_t> allowed{0};
   constexpr int P = BACK ? kBackAhead : kForwardAhead;
   constexpr int kRing = kWarps * P * (BACK ? 2 : 1) * NU * 2 * 32 * V * (int)sizeof(T);
-  auto kernel = qk_rope_kernel<T, V, NU, ADJ, BACK, FULL>;
+  auto kernel = qk_rope_kernel<T, V, NU, PAIRS, BACK, FULL>;
   const cudaError_t e = allow_dynamic_smem(kernel, kRing + kWarps * (P + 1) * STAGE_MAX_HEAD_DIM * 4, allowed);
   if (e != cudaSuccess) return e;
   return launch_dependent(kernel, (unsigned)(a.side[0].blocks + a.side[1].blocks), kThreads, kRing + kWarps * (P + 1) * a.table_bytes, stream, 1, a);
 }
 
-template <typename T, bool ADJ, bool BACK>
+template <typename T, Pairs PAIRS, bool BACK>
 cudaError_t launch_width(const RopeArgs &a, int v, cudaStream_t stream) {
   // whole heads that turn, with as many units as lanes, are the common case: they need no choices
   constexpr int kWide = 16 / (int)sizeof(T);
-  if (v == kWide && a.rot == a.d && (a.d / (2 * kWide) & (a.d / (2 * kWide) - 1)) == 0) return launch_unit<T, kWide, 1, ADJ, BACK, true>(a, stream);
+  if (v == kWide && a.rot == a.d && (a.d / (2 * kWide) & (a.d / (2 * kWide) - 1)) == 0) return launch_unit<T, kWide, 1, PAIRS, BACK, true>(a, stream);
   if constexpr (sizeof(T) == 2) {
-    if (v == 8) return launch_unit<T, 8, 1, ADJ, BACK>(a, stream);
+    if (v == 8) return launch_unit<T, 8, 1, PAIRS, BACK>(a, stream);
   }
-  if (v >= 4) return launch_unit<T, 4, 1, ADJ, BACK>(a, stream);
-  if (v == 2) return launch_unit<T, 2, 2, ADJ, BACK>(a, stream);
-  return launch_unit<T, 1, 4, ADJ, BACK>(a, stream);
-}
-
-template <bool BACK>
-ssn_status_t launch_rope(const stage_qk_rope_t *op, RopeArgs &a, int v, cudaStream_t stream) {
-  const bool adj = op->pairing == STAGE_PAIR_ADJACENT;
-  cudaError_t e;
-  if (op->dtype == SSN_F32)
-    e = adj ? launch_width<float, true, BACK>(a, v, stream) : launch_width<float, false, BACK>(a, v, stream);
-  else
-    e = adj ? launch_width<__nv_bfloat16, true, BACK>(a, v, stream) : launch_width<__nv_bfloat16, false, BACK>(a, v, stream);
-  return launched(e);
+  if (v >= 4) return launch_unit<T, 4, 1, PAIRS, BACK>(a, stream);
+  if (v == 2) return launch_unit<T, 2, 2, PAIRS, BACK>(a, stream);
+  return launch_unit<T, 1, 4, PAIRS, BACK>(a, stream);
 }
 
 // Lanes per row and the blocks of both sides
@@ -549,15 +601,11 @@ void fill(const stage_qk_rope_t *op, RopeArgs &a, const int32_t *pos, int64_t n,
   a.side[1].w = op->wk;
 }
 
-int width_of(const stage_qk_rope_t *op, const RopeArgs &a, bool back) {
+// The width, and how pairs come together
+int width_of(const stage_qk_rope_t *op, const RopeArgs &a, bool back, Pairs &pairs) {
   const size_t item = op->dtype == SSN_F32 ? 4 : 2;
   Width w(item);
-  if (op->pairing == STAGE_PAIR_ADJACENT) {
-    w.stride(a.d / 2);
-  } else {
-    w.stride(a.rot / 2);
-    w.stride((a.d - a.rot) / 2);
-  }
+  w.stride(a.d / 2);
   for (const RopeSide &s : a.side) {
     if (s.heads == 0) continue;
     w.address(s.x, item);
@@ -570,7 +618,33 @@ int width_of(const stage_qk_rope_t *op, const RopeArgs &a, bool back) {
       w.stride(s.dy_head);
     }
   }
-  return w.v;
+  pairs = op->pairing == STAGE_PAIR_ADJACENT ? ADJACENT : HALVES;
+  if (pairs == ADJACENT) return w.v;
+  Width together = w;
+  together.stride(a.rot / 2);
+  together.stride((a.d - a.rot) / 2);
+  // Units of fewer than four pairs are left to CROSSED where the rows allow wide pieces.  16384 x 40 heads of 128, bf16, 98 columns
+  // turned (one pair per unit): 304 / 413 us forward and back, crossed 92 / 137; 100 columns (two) 161 / 251 and 81 / 137; 104 (four) 83 / 117
+  // and 100 / 141.  The gradients take pieces of four: with eight their registers spill (183 us).
+  if (together.v < 4 && w.v >= 4) {
+    pairs = CROSSED;
+    return back ? 4 : w.v;
+  }
+  return together.v;
+}
+
+template <typename T, bool BACK>
+cudaError_t launch_pairs(const RopeArgs &a, Pairs pairs, int v, cudaStream_t stream) {
+  if constexpr (sizeof(T) == 2 && !BACK) {
+    if (pairs == CROSSED && v == 8) return launch_unit<T, 8, 1, CROSSED, BACK>(a, stream);
+  }
+  if (pairs == CROSSED) return launch_unit<T, 4, 1, CROSSED, BACK>(a, stream);
+  return pairs == ADJACENT ? launch_width<T, ADJACENT, BACK>(a, v, stream) : launch_width<T, HALVES, BACK>(a, v, stream);
+}
+
+template <bool BACK>
+ssn_status_t launch_rope(const stage_qk_rope_t *op, const RopeArgs &a, Pairs pairs, int v, cudaStream_t stream) {
+  return launched(op->dtype == SSN_F32 ? launch_pairs<float, BACK>(a, pairs, v, stream) : launch_pairs<__nv_bfloat16, BACK>(a, pairs, v, stream));
 }
 
 }  // namespace
@@ -615,9 +689,10 @@ ssn_status_t stage_qk_rope_forward(const stage_qk_rope_t *op, const void *q, int
   const RopeSide ks{k, nullptr, k_out, op->wk, nullptr, k_token, k_head, 0, 0, ko_token, ko_head, k_heads, 0, 1, 1};
   a.side[0] = qs;
   a.side[1] = ks;
-  const int v = width_of(op, a, false);
+  Pairs pairs;
+  const int v = width_of(op, a, false, pairs);
   plan(op, a, v);
-  return launch_rope<false>(op, a, v, static_cast<cudaStream_t>(stream));
+  return launch_rope<false>(op, a, pairs, v, static_cast<cudaStream_t>(stream));
 }
 
 // Partial sums of at most the resident blocks, D floats each (a side never has fewer than a slot per part of its heads)
@@ -663,12 +738,13 @@ ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, i
     const RopeSide ks{k, dk, dk_in, op->wk, nullptr, k_token, k_head, dk_token, dk_head, dki_token, dki_head, k_heads, 0, 1, 1};
     a.side[0] = qs;
     a.side[1] = ks;
-    const int v = width_of(op, a, true);
+    Pairs pairs;
+    const int v = width_of(op, a, true, pairs);
     plan(op, a, v);
     float *partial = static_cast<float *>(workspace);
     if (dwq != nullptr) a.side[0].partial = partial;
     if (dwk != nullptr) a.side[1].partial = partial + (int64_t)a.side[0].blocks * d;
-    if ((st = launch_rope<true>(op, a, v, s)) != SSN_OK) return st;
+    if ((st = launch_rope<true>(op, a, pairs, v, s)) != SSN_OK) return st;
   }
   if (dwq != nullptr || dwk != nullptr) {
     GainArgs g{{a.side[0].partial, a.side[1].partial}, {dwq, dwk}, {a.side[0].blocks, a.side[1].blocks}, d};

@@ -84,6 +84,17 @@ CASES = [
     (50, 2, 1, 20, 12, "bf16", "adjacent", "heads", True),
     (50, 40, 0, 192, 128, "bf16", "halves", "packed", True),
     (50, 0, 5, 112, 48, "f32", "adjacent", "plain", False),
+    # halves at distances that no wide piece divides
+    (130, 7, 2, 128, 98, "bf16", "halves", "packed", True),
+    (65, 3, 1, 80, 34, "bf16", "halves", "heads", False),
+    (21, 5, 2, 256, 2, "bf16", "halves", "plain", True),
+    (21, 5, 2, 256, 254, "f32", "halves", "plain", True),
+    (33, 2, 1, 96, 30, "f32", "halves", "packed", True),
+    (301, 6, 1, 72, 36, "bf16", "halves", "plain", False),
+    (11, 3, 2, 24, 22, "bf16", "halves", "plain", True),
+    (11, 3, 2, 8, 6, "f32", "halves", "heads", True),
+    (77, 9, 3, 128, 98, "bf16", "adjacent", "heads", True),
+    (77, 9, 3, 72, 70, "f32", "adjacent", "packed", False),
 ]
 
 
