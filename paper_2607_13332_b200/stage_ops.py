@@ -19,6 +19,7 @@ _CODES = {torch.float32: binding.SSN_F32, torch.bfloat16: binding.SSN_BF16}
 # against 1.8 to 3.5 us for torch.empty.
 _current_device = torch._C._cuda_getDevice
 _new = torch._C._dynamo.guards._empty_strided_cuda
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _here(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:
@@ -36,6 +37,19 @@ def _pitch(t: torch.Tensor, rows: int, cols: int) -> int:
     if (unit != 1 and cols > 1) or (rows > 1 and ld < cols):     # rows that share elements have no leading dimension
         raise ValueError("expected a row-major 2-D tensor (unit stride along the last dimension)")
     return ld if rows > 1 else cols
+
+
+def _matrix(t: torch.Tensor, dtype: torch.dtype, device: int, what: str) -> Tuple[int, int, int, int]:
+    """(rows, columns, address, leading dimension) of a row-major matrix of that type on that device."""
+    if t.get_device() != device:
+        raise ValueError(f"{what}: expected a CUDA tensor on the current device")
+    if t.dtype is not dtype:
+        raise ValueError(f"{what}: expected {dtype}, got {t.dtype}")
+    rows, cols = t.shape
+    ld, unit = t.stride()
+    if (unit != 1 and cols > 1) or (rows > 1 and ld < cols):
+        raise ValueError(f"{what}: expected a row-major 2-D tensor (unit stride along the last dimension)")
+    return rows, cols, t.data_ptr(), ld if rows > 1 else cols
 
 
 def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) -> int:
@@ -82,51 +96,54 @@ class QKNormRope:
         self.dev_status.zero_()
         return v
 
-    def _heads(self, t: Optional[torch.Tensor], n: int, heads: int, what: str):
-        """(address, token stride, head stride) of a [n, heads, head_dim] tensor, or of an absent one."""
+    def _rows(self, some: Optional[torch.Tensor]) -> int:
+        """Number of tokens of the tensor that tells it; the operator's device has to be the current one."""
+        if some is None:
+            raise ValueError("neither queries nor keys")
+        if _current_device() != self._device:     # its stream is the one that the kernel is put on
+            raise ValueError("the current device is not the operator's")
+        if some.dim() != 3:
+            raise ValueError("expected [tokens, heads, head_dim]")
+        return some.shape[0]
+
+    def _heads(self, t: Optional[torch.Tensor], n: int, what: str, heads: int = -1):
+        """(address, token stride, head stride, heads) of a [n, heads, head_dim] tensor, or of an absent one."""
         if t is None:
-            if n * heads:
+            if n * heads > 0:
                 raise ValueError(f"{what} is missing")
-            return 0, 0, 0
-        if t.dtype != self.dtype or t.get_device() != self._device:
+            return 0, 0, 0, 0
+        if t.dtype is not self.dtype or t.get_device() != self._device:
             raise ValueError(f"{what}: expected {self.dtype} on the operator's device")
-        if t.shape != (n, heads, self.head_dim):
-            raise ValueError(f"{what}: expected [{n}, {heads}, {self.head_dim}]")
+        rows, count, d = t.shape
+        if rows != n or d != self.head_dim or (count != heads and heads >= 0):
+            raise ValueError(f"{what}: expected [{n}, {heads if heads >= 0 else 'heads'}, {self.head_dim}]")
         token, head, unit = t.stride()
         if unit != 1:
             raise ValueError(f"{what}: expected unit stride along the last dimension")
-        return t.data_ptr(), token, head
+        return t.data_ptr(), token, head, count
 
     def _out(self, t: Optional[torch.Tensor], n: int, heads: int, absent: bool, what: str):
-        """The output tensor, made here unless it is given, and its (address, token stride, head stride)."""
+        """The output tensor, made here unless it is given, with its address, token stride and head stride."""
         if t is not None:
-            return t, self._heads(t, n, heads, what)
+            return t, *self._heads(t, n, what, heads)[:3]
         if absent:
-            return None, (0, 0, 0)
+            return None, 0, 0, 0
         d = self.head_dim
-        t = _new((n, heads, d), (heads * d, d, 1), self.dtype)
-        return t, (t.data_ptr(), heads * d, d)
-
-    def _sizes(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor]) -> Tuple[int, int, int]:
-        some = q if q is not None else k
-        if some is None:
-            raise ValueError("neither queries nor keys")
-        if some.dim() != 3:
-            raise ValueError("expected [tokens, heads, head_dim]")
-        if _current_device() != self._device:     # its stream is the one that the kernel is put on
-            raise ValueError("the current device is not the operator's")
-        return some.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+        pitch = heads * d
+        t = _new((n, heads, d), (pitch, d, 1), self.dtype)
+        return t, t.data_ptr(), pitch, d
 
     def forward(self, q: Optional[torch.Tensor], k: Optional[torch.Tensor], pos: Optional[torch.Tensor] = None, seq_len: int = 0,
                 q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
         """q [n, q_heads, head_dim] and k [n, k_heads, head_dim] (views of any strides; either may be None), normed and rotated.
         Positions: pos int32[n], or t mod seq_len.  An output given may be its input.  Returns (q_out, k_out)."""
-        n, qh, kh = self._sizes(q, k)
-        qa, ka = self._heads(q, n, qh, "q"), self._heads(k, n, kh, "k")
-        q_out, qo = self._out(q_out, n, qh, q is None, "q_out")
-        k_out, ko = self._out(k_out, n, kh, k is None, "k_out")
-        st = _lib.stage_qk_rope_forward(self._ref, *qa, qh, *ka, kh, *qo, *ko, _vector(pos, n, torch.int32, "pos"), n, seq_len,
-                                        _stream())
+        n = self._rows(k if q is None else q)
+        qa, qt, qs, qh = self._heads(q, n, "q")
+        ka, kt, ks, kh = self._heads(k, n, "k")
+        q_out, qoa, qot, qos = self._out(q_out, n, qh, q is None, "q_out")
+        k_out, koa, kot, kos = self._out(k_out, n, kh, k is None, "k_out")
+        st = _lib.stage_qk_rope_forward(self._ref, qa, qt, qs, qh, ka, kt, ks, kh, qoa, qot, qos, koa, kot, kos,
+                                        _vector(pos, n, torch.int32, "pos"), n, seq_len, _raw_stream(self._device))
         if st:
             binding.check(st, "stage_qk_rope_forward")
         return q_out, k_out
@@ -136,11 +153,13 @@ class QKNormRope:
                  dk_in: Optional[torch.Tensor] = None, gains: bool = True):
         """From the gradients of forward's outputs and forward's inputs: (dq_in, dk_in, dwq, dwk), the gains' gradients in
         fp32 [head_dim], or None without `gains`.  dq_in may be dq, dk_in dk."""
-        n, qh, kh = self._sizes(q, k)
-        dqa, dka = self._heads(dq, n, qh, "dq"), self._heads(dk, n, kh, "dk")
-        qa, ka = self._heads(q, n, qh, "q"), self._heads(k, n, kh, "k")
-        dq_in, dqo = self._out(dq_in, n, qh, q is None, "dq_in")
-        dk_in, dko = self._out(dk_in, n, kh, k is None, "dk_in")
+        n = self._rows(k if q is None else q)
+        qa, qt, qs, qh = self._heads(q, n, "q")
+        ka, kt, ks, kh = self._heads(k, n, "k")
+        dqa, dqt, dqs, _ = self._heads(dq, n, "dq", qh)
+        dka, dkt, dks, _ = self._heads(dk, n, "dk", kh)
+        dq_in, dqoa, dqot, dqos = self._out(dq_in, n, qh, q is None, "dq_in")
+        dk_in, dkoa, dkot, dkos = self._out(dk_in, n, kh, k is None, "dk_in")
         dwq = dwk = scratch = None
         nbytes = 0
         if gains:
@@ -150,8 +169,9 @@ class QKNormRope:
                 nbytes = self._workspace[qh, kh] = _lib.stage_qk_rope_workspace_bytes(self._ref, 1, qh, kh)
             dwq, dwk = _new((d,), (1,), torch.float32), _new((d,), (1,), torch.float32)
             scratch = _new((nbytes,), (1,), torch.uint8)      # one per call: captured calls share none
-        st = _lib.stage_qk_rope_backward(self._ref, *dqa, *dka, *qa, qh, *ka, kh, *dqo, *dko, _ptr(dwq), _ptr(dwk),
-                                         _vector(pos, n, torch.int32, "pos"), n, seq_len, _ptr(scratch), nbytes, _stream())
+        st = _lib.stage_qk_rope_backward(self._ref, dqa, dqt, dqs, dka, dkt, dks, qa, qt, qs, qh, ka, kt, ks, kh, dqoa, dqot, dqos,
+                                         dkoa, dkot, dkos, _ptr(dwq), _ptr(dwk), _vector(pos, n, torch.int32, "pos"), n, seq_len,
+                                         _ptr(scratch), nbytes, _raw_stream(self._device))
         if st:
             binding.check(st, "stage_qk_rope_backward")
         return dq_in, dk_in, dwq, dwk
@@ -164,19 +184,21 @@ def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight:
     code = _CODES.get(dtype)
     if code is None:
         raise ValueError("logits: expected fp32 or bf16")
-    n, vocab = _here(logits, dtype, "logits").shape
-    rows, top_k = _here(ids, torch.int32, "ids").shape
-    if _here(top, torch.float32, "top").shape != (rows, top_k) or rows != n:
+    device = _current_device()
+    n, vocab, at, ldl = _matrix(logits, dtype, device, "logits")
+    rows, top_k, ids_at, ldi = _matrix(ids, torch.int32, device, "ids")
+    top_rows, top_cols, top_at, ldt = _matrix(top, torch.float32, device, "top")
+    if rows != n or top_rows != n or top_cols != top_k:
         raise ValueError(f"ids, top: expected [{n}, top_k] each")
     out, ldd = 0, 0
     if dlogits is not None:
-        if _here(dlogits, dtype, "dlogits").shape != (n, vocab):
+        out_rows, out_cols, out, ldd = _matrix(dlogits, dtype, device, "dlogits")
+        if out_rows != n or out_cols != vocab:
             raise ValueError("dlogits: expected the shape of the logits")
-        out, ldd = dlogits.data_ptr(), _pitch(dlogits, n, vocab)
     loss = _new((n,), (1,), torch.float32)
-    st = _lib.stage_distill_loss(logits.data_ptr(), _pitch(logits, n, vocab), code, n, vocab, ids.data_ptr(), _pitch(ids, n, top_k),
-                                 top.data_ptr(), _pitch(top, n, top_k), top_k, _vector(weight, n, torch.float32, "weight"), temperature,
-                                 loss.data_ptr(), out, ldd, _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
+    st = _lib.stage_distill_loss(at, ldl, code, n, vocab, ids_at, ldi, top_at, ldt, top_k, _vector(weight, n, torch.float32, "weight"),
+                                 temperature, loss.data_ptr(), out, ldd, _vector(dev_status, 1, torch.int32, "dev_status"),
+                                 _raw_stream(device))
     if st:
         binding.check(st, "stage_distill_loss")
     return loss
@@ -206,16 +228,18 @@ def int8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None):
     code = _CODES.get(x.dtype)
     if code is None:
         raise ValueError("x: expected fp32 or bf16")
-    rows, cols = _here(x, x.dtype, "x").shape
+    device = _current_device()
+    rows, cols, at, ldx = _matrix(x, x.dtype, device, "x")
     if q is None:
         ldq = cols + (-cols & 15)
         q = _new((rows, cols), (ldq, 1), torch.int8)
-    elif _here(q, torch.int8, "q").shape != (rows, cols):
-        raise ValueError("q: expected the shape of x")
+        q_at = q.data_ptr()
     else:
-        ldq = _pitch(q, rows, cols)
+        q_rows, q_cols, q_at, ldq = _matrix(q, torch.int8, device, "q")
+        if q_rows != rows or q_cols != cols:
+            raise ValueError("q: expected the shape of x")
     scale = _new((rows,), (1,), torch.float32)
-    st = _lib.stage_int8_quantize(x.data_ptr(), _pitch(x, rows, cols), code, rows, cols, q.data_ptr(), ldq, scale.data_ptr(), _stream())
+    st = _lib.stage_int8_quantize(at, ldx, code, rows, cols, q_at, ldq, scale.data_ptr(), _raw_stream(device))
     if st:
         binding.check(st, "stage_int8_quantize")
     return q, scale
@@ -224,20 +248,22 @@ def int8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None):
 def int8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, dtype: str = "bf16",
                 out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y [n, outer] of dtype = (xq [n, inner] times wq [outer, inner] transposed), scaled by xs [n] and ws [outer]."""
-    n, inner = _here(xq, torch.int8, "xq").shape
-    outer, depth = _here(wq, torch.int8, "wq").shape
+    device = _current_device()
+    n, inner, x_at, ldx = _matrix(xq, torch.int8, device, "xq")
+    outer, depth, w_at, ldw = _matrix(wq, torch.int8, device, "wq")
     if depth != inner:
         raise ValueError(f"wq: expected [outer, {inner}]")
     kind = _TORCH_DTYPE[dtype]
     if out is None:
         out, ldy = _new((n, outer), (outer, 1), kind), outer
-    elif _here(out, kind, "out").shape != (n, outer):
-        raise ValueError(f"out: expected [{n}, {outer}]")
+        y_at = out.data_ptr()
     else:
-        ldy = _pitch(out, n, outer)
-    st = _lib.stage_int8_matmul(xq.data_ptr(), _pitch(xq, n, inner), _vector(xs, n, torch.float32, "xs"), wq.data_ptr(),
-                                _pitch(wq, outer, inner), _vector(ws, outer, torch.float32, "ws"), n, inner, outer, out.data_ptr(), ldy,
-                                _CODES[kind], _vector(dev_status, 1, torch.int32, "dev_status"), _stream())
+        rows, cols, y_at, ldy = _matrix(out, kind, device, "out")
+        if rows != n or cols != outer:
+            raise ValueError(f"out: expected [{n}, {outer}]")
+    st = _lib.stage_int8_matmul(x_at, ldx, _vector(xs, n, torch.float32, "xs"), w_at, ldw, _vector(ws, outer, torch.float32, "ws"),
+                                n, inner, outer, y_at, ldy, _CODES[kind], _vector(dev_status, 1, torch.int32, "dev_status"),
+                                _raw_stream(device))
     if st:
         binding.check(st, "stage_int8_matmul")
     return out
