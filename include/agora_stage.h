@@ -149,6 +149,65 @@ ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, c
                                const float *ws, int64_t n_tokens, int64_t inner, int64_t outer, void *y, int64_t ldy,
                                int32_t dtype, int32_t *dev_status, void *stream);
 
+/* ---- the same calls with their arguments in one struct ---------------------------------------------- */
+
+/*
+ * For callers whose foreign-function layer takes long over each argument (calls of one token are shorter on the GPU than
+ * that): the fields are the arguments of the call of that name, in its order.  `args` is read during the call.
+ */
+typedef struct stage_qk_rope_forward_args {
+  const stage_qk_rope_t *op;
+  const void *q; int64_t q_token, q_head; int32_t q_heads;
+  const void *k; int64_t k_token, k_head; int32_t k_heads;
+  void *q_out; int64_t qo_token, qo_head;
+  void *k_out; int64_t ko_token, ko_head;
+  const int32_t *pos; int64_t n_tokens; int32_t seq_len; void *stream;
+} stage_qk_rope_forward_args_t;
+
+typedef struct stage_qk_rope_backward_args {
+  const stage_qk_rope_t *op;
+  const void *dq; int64_t dq_token, dq_head;
+  const void *dk; int64_t dk_token, dk_head;
+  const void *q; int64_t q_token, q_head; int32_t q_heads;
+  const void *k; int64_t k_token, k_head; int32_t k_heads;
+  void *dq_in; int64_t dqi_token, dqi_head;
+  void *dk_in; int64_t dki_token, dki_head;
+  float *dwq, *dwk;
+  const int32_t *pos; int64_t n_tokens; int32_t seq_len;
+  void *workspace; size_t workspace_bytes; void *stream;
+} stage_qk_rope_backward_args_t;
+
+typedef struct stage_distill_loss_args {
+  const void *logits; int64_t ldl; int32_t dtype; int64_t n_tokens, vocab;
+  const int32_t *ids; int64_t ldi;
+  const float *top; int64_t ldt; int32_t top_k;
+  const float *weight; float tau; float *loss;
+  void *dlogits; int64_t ldd;
+  int32_t *dev_status; void *stream;
+} stage_distill_loss_args_t;
+
+typedef struct stage_int8_quantize_args {
+  const void *x; int64_t ldx; int32_t dtype; int64_t rows, cols;
+  int8_t *q; int64_t ldq;
+  float *scale; void *stream;
+} stage_int8_quantize_args_t;
+
+typedef struct stage_int8_matmul_args {
+  const int8_t *xq; int64_t ldx;
+  const float *xs;
+  const int8_t *wq; int64_t ldw;
+  const float *ws;
+  int64_t n_tokens, inner, outer;
+  void *y; int64_t ldy; int32_t dtype;
+  int32_t *dev_status; void *stream;
+} stage_int8_matmul_args_t;
+
+ssn_status_t stage_qk_rope_forward_packed(const stage_qk_rope_forward_args_t *args);
+ssn_status_t stage_qk_rope_backward_packed(const stage_qk_rope_backward_args_t *args);
+ssn_status_t stage_distill_loss_packed(const stage_distill_loss_args_t *args);
+ssn_status_t stage_int8_quantize_packed(const stage_int8_quantize_args_t *args);
+ssn_status_t stage_int8_matmul_packed(const stage_int8_matmul_args_t *args);
+
 #ifdef __cplusplus
 }
 #endif

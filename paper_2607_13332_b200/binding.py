@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes
 import os
 import re
+import struct
 from typing import Optional, Sequence
 
 from . import buildlib
@@ -134,6 +135,10 @@ _SIGNATURES = {
     "ssn_last_kernel": (_i32, []),
     "ssn_selftest_bounded_wait": (_i32, [_i32, _vp, _vp]),
 }
+# calls whose arguments may also be handed over as one struct
+_PACKED = ("stage_qk_rope_forward", "stage_qk_rope_backward", "stage_distill_loss", "stage_int8_quantize", "stage_int8_matmul")
+_SIGNATURES.update({_name + "_packed": (_i32, [ctypes.c_char_p]) for _name in _PACKED})
+_FORMAT = {_vp: "P", _rope_p: "P", _i64: "q", _i32: "i", _sz: "N", ctypes.c_float: "f"}
 for _name, (_res, _args) in _SIGNATURES.items():
     _fn = getattr(_lib, _name)
     _fn.restype, _fn.argtypes = _res, _args
@@ -344,6 +349,11 @@ def ssn_prepare_tables(codec: ssn_codec_t, EU: int, ldeu: int, PU: int, ldpu: in
 def library() -> ctypes.CDLL:
     """The loaded library: its functions return the status instead of raising; 0 is NULL."""
     return _lib
+
+
+def packed(name: str):
+    """(call, pack) of a call in _PACKED: call(pack(its arguments)) returns its status.  Pointers are addresses, 0 is NULL."""
+    return getattr(_lib, name + "_packed"), struct.Struct("@" + "".join(_FORMAT[t] for t in _SIGNATURES[name][1])).pack
 
 
 check = _check   # raises SsnError for a status other than SSN_OK

@@ -3,7 +3,7 @@ runs in the library's kernels, on the current stream of the current device."""
 
 from __future__ import annotations
 
-from ctypes import byref
+from ctypes import addressof, byref
 from typing import Optional, Tuple
 
 import torch
@@ -12,6 +12,12 @@ from . import binding
 from .runner import _TORCH_DTYPE, _ptr, _stream
 
 _lib = binding.library()
+# ctypes converts every argument of a call, which takes as long as a launch; one block of bytes does not
+_forward, _forward_args = binding.packed("stage_qk_rope_forward")
+_backward, _backward_args = binding.packed("stage_qk_rope_backward")
+_loss, _loss_args = binding.packed("stage_distill_loss")
+_quantize, _quantize_args = binding.packed("stage_int8_quantize")
+_matmul, _matmul_args = binding.packed("stage_int8_matmul")
 _CODES = {torch.float32: binding.SSN_F32, torch.bfloat16: binding.SSN_BF16}
 
 # Calls of one token are shorter on the GPU than on the host, so every call asks each tensor once for its type, device, shape
@@ -87,7 +93,7 @@ class QKNormRope:
         self._device = _here(self.dev_status, torch.int32, "device").get_device()     # calls are for this device alone
         self.c = binding.make_qk_rope(head_dim, rot, binding.DTYPES[dtype], binding.PAIRINGS[pairing], eps, _ptr(wq), _ptr(wk),
                                       _ptr(table), _pitch(table, max_pos, rot) if table is not None else 0, max_pos, self.dev_status.data_ptr())
-        self._ref = byref(self.c)
+        self._ref, self._address = byref(self.c), addressof(self.c)
         self._workspace = {}
 
     def take_status(self) -> int:
@@ -142,8 +148,8 @@ class QKNormRope:
         ka, kt, ks, kh = self._heads(k, n, "k")
         q_out, qoa, qot, qos = self._out(q_out, n, qh, q is None, "q_out")
         k_out, koa, kot, kos = self._out(k_out, n, kh, k is None, "k_out")
-        st = _lib.stage_qk_rope_forward(self._ref, qa, qt, qs, qh, ka, kt, ks, kh, qoa, qot, qos, koa, kot, kos,
-                                        _vector(pos, n, torch.int32, "pos"), n, seq_len, _raw_stream(self._device))
+        st = _forward(_forward_args(self._address, qa, qt, qs, qh, ka, kt, ks, kh, qoa, qot, qos, koa, kot, kos,
+                                    _vector(pos, n, torch.int32, "pos"), n, seq_len, _raw_stream(self._device)))
         if st:
             binding.check(st, "stage_qk_rope_forward")
         return q_out, k_out
@@ -169,9 +175,9 @@ class QKNormRope:
                 nbytes = self._workspace[qh, kh] = _lib.stage_qk_rope_workspace_bytes(self._ref, 1, qh, kh)
             dwq, dwk = _new((d,), (1,), torch.float32), _new((d,), (1,), torch.float32)
             scratch = _new((nbytes,), (1,), torch.uint8)      # one per call: captured calls share none
-        st = _lib.stage_qk_rope_backward(self._ref, dqa, dqt, dqs, dka, dkt, dks, qa, qt, qs, qh, ka, kt, ks, kh, dqoa, dqot, dqos,
-                                         dkoa, dkot, dkos, _ptr(dwq), _ptr(dwk), _vector(pos, n, torch.int32, "pos"), n, seq_len,
-                                         _ptr(scratch), nbytes, _raw_stream(self._device))
+        st = _backward(_backward_args(self._address, dqa, dqt, dqs, dka, dkt, dks, qa, qt, qs, qh, ka, kt, ks, kh, dqoa, dqot, dqos,
+                                      dkoa, dkot, dkos, _ptr(dwq), _ptr(dwk), _vector(pos, n, torch.int32, "pos"), n, seq_len,
+                                      _ptr(scratch), nbytes, _raw_stream(self._device)))
         if st:
             binding.check(st, "stage_qk_rope_backward")
         return dq_in, dk_in, dwq, dwk
@@ -196,9 +202,9 @@ def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight:
         if out_rows != n or out_cols != vocab:
             raise ValueError("dlogits: expected the shape of the logits")
     loss = _new((n,), (1,), torch.float32)
-    st = _lib.stage_distill_loss(at, ldl, code, n, vocab, ids_at, ldi, top_at, ldt, top_k, _vector(weight, n, torch.float32, "weight"),
-                                 temperature, loss.data_ptr(), out, ldd, _vector(dev_status, 1, torch.int32, "dev_status"),
-                                 _raw_stream(device))
+    st = _loss(_loss_args(at, ldl, code, n, vocab, ids_at, ldi, top_at, ldt, top_k, _vector(weight, n, torch.float32, "weight"),
+                          temperature, loss.data_ptr(), out, ldd, _vector(dev_status, 1, torch.int32, "dev_status"),
+                          _raw_stream(device)))
     if st:
         binding.check(st, "stage_distill_loss")
     return loss
@@ -239,7 +245,7 @@ def int8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None):
         if q_rows != rows or q_cols != cols:
             raise ValueError("q: expected the shape of x")
     scale = _new((rows,), (1,), torch.float32)
-    st = _lib.stage_int8_quantize(at, ldx, code, rows, cols, q_at, ldq, scale.data_ptr(), _raw_stream(device))
+    st = _quantize(_quantize_args(at, ldx, code, rows, cols, q_at, ldq, scale.data_ptr(), _raw_stream(device)))
     if st:
         binding.check(st, "stage_int8_quantize")
     return q, scale
@@ -261,9 +267,9 @@ def int8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.
         rows, cols, y_at, ldy = _matrix(out, kind, device, "out")
         if rows != n or cols != outer:
             raise ValueError(f"out: expected [{n}, {outer}]")
-    st = _lib.stage_int8_matmul(x_at, ldx, _vector(xs, n, torch.float32, "xs"), w_at, ldw, _vector(ws, outer, torch.float32, "ws"),
-                                n, inner, outer, y_at, ldy, _CODES[kind], _vector(dev_status, 1, torch.int32, "dev_status"),
-                                _raw_stream(device))
+    st = _matmul(_matmul_args(x_at, ldx, _vector(xs, n, torch.float32, "xs"), w_at, ldw, _vector(ws, outer, torch.float32, "ws"),
+                              n, inner, outer, y_at, ldy, _CODES[kind], _vector(dev_status, 1, torch.int32, "dev_status"),
+                              _raw_stream(device)))
     if st:
         binding.check(st, "stage_int8_matmul")
     return out
