@@ -143,10 +143,12 @@ __device__ __forceinline__ double log_of(float x) {
 }
 
 // What some of the teacher's entries contribute: their largest logit, the sum of e = exp((top - m) / tau), and the sum of
-// e (top - s) over those whose column is at hand.  The last one is a difference of large terms in the end: 64 bits.
+// e (top - s) over those whose column is at hand.  The quotient of the two sums is a mean of numbers that may all be large (logits are
+// as good with any constant added), from which as large a one is taken: both are sums of the same fp32 terms in 64 bits, so that
+// the weights of the mean add up to 1.
 struct Teacher {
-  float m, sum;
-  double a;
+  float m;
+  double sum, a;
 };
 
 // Resident CTAs of `threads`: what leaves the pieces in flight in registers
@@ -279,8 +281,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
     if (warp * 32 < a.top_k) {   // the warp's entries
       if (tid < a.top_k) sh.at[tid] = own_at;
       for (int o = 16; o > 0; o >>= 1) tm = fmaxf(tm, __shfl_xor_sync(0xffffffffu, tm, o));
-      float sum = 0.f;
-      double sa = 0.0;
+      double sum = 0.0, sa = 0.0;
       for (int j = tid; j < a.top_k; j += kThreads) {
         const float v = sh.e[j];
         float e = 0.f;
@@ -288,7 +289,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
           e = expf((v - tm) * inv_tau);
           if (sh.id[j] >= 0 && !(e == 0.f)) sa += (double)e * ((double)v - (double)sh.at[j]);
         }
-        sum += e;
+        sum += (double)e;
         sh.e[j] = e;
       }
       for (int o = 16; o > 0; o >>= 1) {
@@ -301,13 +302,13 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
     MaxSum ms = merge_warp(lane < kWarps ? sh.ms[lane] : MaxSum{-INFINITY, 0.f}, scale);
     // the teacher's row: the warps' shares, one after the other
     const int tw = min(kWarps, (a.top_k + 31) / 32);
-    float top_m = sh.teacher[0].m, tsum = 0.f;
-    double ta = 0.0;
+    float top_m = sh.teacher[0].m;
+    double tsum = 0.0, ta = 0.0;
     for (int i = 1; i < tw; ++i) top_m = fmaxf(top_m, sh.teacher[i].m);
     auto share = [&](int i) { return sh.teacher[i].m == -INFINITY ? 0.f : expf((sh.teacher[i].m - top_m) * inv_tau); };
     for (int i = 0; i < tw; ++i) {
       const float f = share(i);
-      tsum += sh.teacher[i].sum * f;
+      tsum += sh.teacher[i].sum * (double)f;
       ta += sh.teacher[i].a * (double)f;
     }
     if (cluster > 1) {
@@ -328,11 +329,11 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
     if (tid == 0 && rank == 0) {
       // log p = (top - top_m) / tau - log tsum, the student's log sum is m / tau + log l
       const double tau = (double)a.tau;
-      const double r0 = (double)(1.f / tsum), r1 = r0 * (2.0 - (double)tsum * r0);   // 1 / tsum: a division in 64 bits takes long
-      a.loss[t] = (float)((double)w * tau * (ta * r1 - (double)top_m + (double)ms.m + tau * (log_of(ms.l) - log_of(tsum))));
+      const double r0 = (double)(1.f / (float)tsum), r1 = r0 * (2.0 - tsum * r0);   // 1 / tsum to 2^-45: a division in 64 bits takes long
+      a.loss[t] = (float)((double)w * tau * (ta * r1 - (double)top_m + (double)ms.m + tau * (log_of(ms.l) - log_of((float)tsum))));
     }
     if (GRAD) {
-      const float c = w * a.tau / ms.l;
+      const float c = w * a.tau / ms.l, sum_p = (float)tsum;
       auto put = [&](Piece<T> &v, int i) {
         v.to_gradient(ms.m, scale, c);
         if (same) v.store(dst + (int64_t)i * 16);
@@ -371,7 +372,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
           p += __shfl_xor_sync(0xffffffffu, p, o);
           first = __shfl_xor_sync(0xffffffffu, (int)first, o) != 0 && first;
         }
-        if ((tid & 7) == 0 && id >= 0 && first) out[id] = from_f32<T>(exp2_approx((sh.at[j] - ms.m) * scale) * c - w * a.tau * (p / tsum));
+        if ((tid & 7) == 0 && id >= 0 && first) out[id] = from_f32<T>(exp2_approx((sh.at[j] - ms.m) * scale) * c - w * a.tau * (p / sum_p));
       }
     }
   }
