@@ -42,3 +42,14 @@ def test_a_constant_added_to_the_teacher_or_the_student(n, vocab, k, dtype, tau,
         logits = logits + shift / 2
         loss, grad = distill_loss_grad(logits, ids, top, weight, temperature=tau)
         assert_rows(logits, ids, top, weight, tau, loss, grad, far=2 * abs(shift))
+
+
+@pytest.mark.parametrize("vocab", [4000, 4001])
+def test_last_tokens_of_sequences(vocab):
+    """A view whose rows are far apart: the gradient made for it holds its rows alone."""
+    rng = np.random.default_rng(vocab)
+    logits, ids, top, weight = make(rng, 24 * 9, vocab, 16, "bf16")
+    last = logits.view(24, 9, vocab)[:, -1]
+    loss, grad = distill_loss_grad(last, ids[:24], top[:24], weight[:24])
+    assert_rows(last, ids[:24], top[:24], weight[:24], 1.0, loss, grad)
+    assert grad.untyped_storage().nbytes() <= 24 * (vocab + 8) * 2

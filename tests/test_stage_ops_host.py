@@ -1,0 +1,30 @@
+"""What the tensor layer of the stage operators does on the host: no GPU."""
+
+import pytest
+import torch
+
+
+@pytest.fixture
+def host(libssn, monkeypatch):
+    """Tensors on the host pass for tensors of the current device: no call below reaches the library."""
+    stage_ops = pytest.importorskip("paper_2607_13332_b200.stage_ops")
+    monkeypatch.setattr(stage_ops, "_current_device", lambda: -1)
+    monkeypatch.setattr(stage_ops, "_new", lambda shape, strides, dtype: torch.empty_strided(shape, strides, dtype=dtype))
+    return stage_ops
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("vocab", [1, 7, 96, 101])
+def test_a_gradient_takes_no_more_room_than_its_rows(host, monkeypatch, dtype, vocab):
+    monkeypatch.setattr(host, "_distill", lambda *args: None)
+    whole = torch.zeros(5, 64, vocab, dtype=dtype)
+    piece = 16 // dtype.itemsize
+    for logits in (whole[:, -1], whole.flatten(0, 1)[::9], whole.flatten(0, 1), whole[:1, 3], torch.zeros(6, vocab + 13, dtype=dtype)[:, :vocab],
+                   torch.zeros(6, 2, vocab, dtype=dtype)[:, 0], whole[:0, 0]):
+        dlogits = host.distill_loss_grad(logits, None, None)[1]
+        n, pitch = len(logits), dlogits.stride(0)
+        assert dlogits.shape == logits.shape and dlogits.dtype == dtype and dlogits.stride(1) == 1
+        assert vocab <= pitch < vocab + piece
+        assert dlogits.untyped_storage().nbytes() <= n * (vocab + piece) * dtype.itemsize
+        if n > 1:      # whole 16-byte pieces of the one are whole pieces of the other
+            assert (logits.stride(0) - pitch) % piece == 0
