@@ -149,6 +149,13 @@ ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, c
                                const float *ws, int64_t n_tokens, int64_t inner, int64_t outer, void *y, int64_t ldy,
                                int32_t dtype, int32_t *dev_status, void *stream);
 
+/*
+ * A status word for callers that keep none of their own: its device address on the current device (NULL without one), the same
+ * one for the life of the process, 0 at first.  Calls OR their bits into it where it is handed over as dev_status, and only
+ * there; who clears it clears it for all of them.
+ */
+int32_t *stage_status_word(void);
+
 /* ---- the same calls with their arguments in one struct ---------------------------------------------- */
 
 /*

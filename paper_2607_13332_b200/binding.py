@@ -129,6 +129,7 @@ _SIGNATURES = {
                                   _vp, _vp]),
     "stage_int8_quantize": (_i32, [_vp, _i64, _i32, _i64, _i64, _vp, _i64, _vp, _vp]),
     "stage_int8_matmul": (_i32, [_vp, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _i64, _vp, _i64, _i32, _vp, _vp]),
+    "stage_status_word": (_vp, []),
     "ssn_status_string": (ctypes.c_char_p, [_i32]),
     "ssn_version": (_i32, []),
     "ssn_launch_count": (_i64, []),

@@ -67,6 +67,43 @@ def _vector(t: Optional[torch.Tensor], n: int, dtype: torch.dtype, what: str) ->
     return t.data_ptr()
 
 
+# Addresses of the status words of calls that are given none, by device
+_words = {}
+
+
+def _status(given: Optional[torch.Tensor], device: int) -> int:
+    """Address of the status word of a call: the given one, or the library's own."""
+    if given is not None:
+        return _vector(given, 1, torch.int32, "dev_status")
+    at = _words.get(device)
+    if at is None:
+        at = _lib.stage_status_word()
+        if not at:
+            raise RuntimeError("no status word on the current device")
+        _words[device] = at
+    return at
+
+
+class _Word:
+    """One int32 at a device address, as torch.as_tensor takes it."""
+
+    def __init__(self, at: int):
+        self.__cuda_array_interface__ = {"shape": (1,), "typestr": "<i4", "data": (at, False), "version": 3}
+
+
+def take_status() -> int:
+    """Read and clear the current device's status word of the losses and products that are given no dev_status (waits for the
+    device): SSN_DEV_BAD_ID and SSN_DEV_TIMEOUT of every call in this process since the last read.  After SSN_DEV_TIMEOUT a
+    product among them is invalid."""
+    device = _current_device()
+    torch.cuda.synchronize(device)
+    word = torch.as_tensor(_Word(_status(None, device)), device=torch.device("cuda", device))
+    v = int(word.item())
+    word.zero_()
+    torch.cuda.synchronize(device)      # cleared before a later call on any stream may set it
+    return v
+
+
 def rope_table(max_pos: int, rot_dim: int, theta: float = 10000.0, device: str = "cuda") -> torch.Tensor:
     """[max_pos, rot_dim] fp32 rotation table: rot_dim / 2 cosines, then as many sines, of every position's angles."""
     table = torch.empty((max_pos, rot_dim), dtype=torch.float32, device=device)
@@ -203,8 +240,7 @@ def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight:
             raise ValueError("dlogits: expected the shape of the logits")
     loss = _new((n,), (1,), torch.float32)
     st = _loss(_loss_args(at, ldl, code, n, vocab, ids_at, ldi, top_at, ldt, top_k, _vector(weight, n, torch.float32, "weight"),
-                          temperature, loss.data_ptr(), out, ldd, _vector(dev_status, 1, torch.int32, "dev_status"),
-                          _raw_stream(device)))
+                          temperature, loss.data_ptr(), out, ldd, _status(dev_status, device), _raw_stream(device)))
     if st:
         binding.check(st, "stage_distill_loss")
     return loss
@@ -213,7 +249,8 @@ def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight:
 def distill_loss(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight: Optional[torch.Tensor] = None,
                  temperature: float = 1.0, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Loss [n] fp32 of logits [n, vocab] against the teacher's top logits top [n, k] fp32 at ids [n, k] int32 (-1: padding):
-    weight times temperature^2 times the divergence of the student's softmax from the teacher's over its entries."""
+    weight times temperature^2 times the divergence of the student's softmax from the teacher's over its entries.  Ids outside
+    the vocabulary set SSN_DEV_BAD_ID in dev_status (int32 [1]), or in the word that take_status() reads."""
     return _distill(logits, ids, top, weight, temperature, None, dev_status)
 
 
@@ -254,7 +291,8 @@ def int8_quantize(x: torch.Tensor, q: Optional[torch.Tensor] = None):
 
 def int8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.Tensor, dtype: str = "bf16",
                 out: Optional[torch.Tensor] = None, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """y [n, outer] of dtype = (xq [n, inner] times wq [outer, inner] transposed), scaled by xs [n] and ws [outer]."""
+    """y [n, outer] of dtype = (xq [n, inner] times wq [outer, inner] transposed), scaled by xs [n] and ws [outer].  A product that
+    went wrong on the GPU sets SSN_DEV_TIMEOUT in dev_status (int32 [1]), or in the word that take_status() reads."""
     device = _current_device()
     n, inner, x_at, ldx = _matrix(xq, torch.int8, device, "xq")
     outer, depth, w_at, ldw = _matrix(wq, torch.int8, device, "wq")
@@ -269,8 +307,7 @@ def int8_matmul(xq: torch.Tensor, xs: torch.Tensor, wq: torch.Tensor, ws: torch.
         if rows != n or cols != outer:
             raise ValueError(f"out: expected [{n}, {outer}]")
     st = _matmul(_matmul_args(x_at, ldx, _vector(xs, n, torch.float32, "xs"), w_at, ldw, _vector(ws, outer, torch.float32, "ws"),
-                              n, inner, outer, y_at, ldy, _CODES[kind], _vector(dev_status, 1, torch.int32, "dev_status"),
-                              _raw_stream(device)))
+                              n, inner, outer, y_at, ldy, _CODES[kind], _status(dev_status, device), _raw_stream(device)))
     if st:
         binding.check(st, "stage_int8_matmul")
     return out

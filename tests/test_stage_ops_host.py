@@ -28,3 +28,22 @@ def test_a_gradient_takes_no_more_room_than_its_rows(host, monkeypatch, dtype, v
         assert dlogits.untyped_storage().nbytes() <= n * (vocab + piece) * dtype.itemsize
         if n > 1:      # whole 16-byte pieces of the one are whole pieces of the other
             assert (logits.stride(0) - pitch) % piece == 0
+
+
+def test_calls_without_a_status_word_share_the_librarys(host, monkeypatch):
+    """What goes wrong on the device is on record whether it was asked for or not."""
+    seen = []
+    for name in ("_loss", "_matmul"):
+        monkeypatch.setattr(host, name + "_args", lambda *args: args)
+        monkeypatch.setattr(host, name, lambda args: seen.append(args[-2]) and 0)
+    monkeypatch.setattr(host, "_raw_stream", lambda device: 0)
+    monkeypatch.setattr(host, "_words", {-1: 0x7000})
+    own = torch.zeros(1, dtype=torch.int32)
+    x, s = torch.zeros(3, 16, dtype=torch.int8), torch.zeros(3)
+    logits, ids, top = torch.zeros(3, 8), torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, 2)
+    for word, want in ((None, 0x7000), (own, own.data_ptr())):
+        del seen[:]
+        host.int8_matmul(x, s, x, s, dev_status=word)
+        host.distill_loss(logits, ids, top, dev_status=word)
+        host.distill_loss_grad(logits, ids, top, dev_status=word)
+        assert seen == [want] * 3
