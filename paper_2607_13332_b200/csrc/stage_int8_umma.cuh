@@ -84,6 +84,9 @@ template <int CG> __device__ __forceinline__ void int8_commit(uint32_t bar) {
   else
     umma_commit(bar);
 }
+// A wait of whole warps: all lanes go on, or all of them give up, since what follows it takes a converged warp
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity)); }
+
 template <int CG, int BN, bool SWAP, bool RAGGED, typename T>
 __global__ void __launch_bounds__((Int8Config<CG, BN, SWAP, RAGGED>::kThreads), 1)
 int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
@@ -190,7 +193,7 @@ int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
           v[i] = row16(next[i], row, st * kInt8Step + piece * 16, bytes);
         }
         if (st + 1 < step_hi) fetch(st + 1);   // on its way while this one is stored
-        if (!dead && !mbar_wait(empty_bar(slot), parity)) {
+        if (!mbar_wait_warp(empty_bar(slot), parity)) {
           timed_out();
           break;
         }
@@ -306,7 +309,7 @@ int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
         }
         __syncwarp();
       }
-      if (!mbar_wait(acc_full_bar(buf), (uint32_t)((count >> 1) & 1))) {
+      if (!mbar_wait_warp(acc_full_bar(buf), (uint32_t)((count >> 1) & 1))) {
         timed_out();
         break;
       }
