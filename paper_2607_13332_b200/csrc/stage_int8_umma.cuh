@@ -76,11 +76,11 @@ __device__ __forceinline__ void int8_mma(uint32_t d, uint64_t a, uint64_t b, uin
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n}\n"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-// Arrives on the barrier (on both CTAs' for a pair) when every MMA issued so far is done
-template <int CG> __device__ __forceinline__ void int8_commit(uint32_t bar) {
+// Arrives on the barrier (on both CTAs' for a pair, or on those of `ranks`) when every MMA issued so far is done
+template <int CG> __device__ __forceinline__ void int8_commit(uint32_t bar, uint16_t ranks = 3) {
   if constexpr (CG == 2)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+                 ::"r"(bar), "h"(ranks) : "memory");
   else
     umma_commit(bar);
 }
@@ -240,7 +240,9 @@ int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
           }
         }
       }
-      if (dead) {   // no copy may land after the CTA has left
+      // No copy may land after the CTA has left, whoever gave up (the MMAs have waited for all of them if nobody did).  A pair's
+      // copies, its second CTA's too, arrive on the first CTA's barriers.
+      if (CG == 1 || rank == 0 || dead) {
         for (int i = 0; i < S && i < issued; ++i) {
           const int n = issued - 1 - i;
           mbar_wait(full_bar(n % S), (uint32_t)((n / S) & 1));
@@ -279,10 +281,8 @@ int8_umma_kernel(const Int8Args a, const __grid_constant__ Int8Maps maps) {
         }
         if (!dead) int8_commit<CG>(acc_full_bar(buf));
       }
-      if (dead) {
-        int8_commit<CG>(drain_bar);
-        mbar_wait(drain_bar, 0);
-      }
+      int8_commit<CG>(drain_bar, 1);   // and no MMA may be under way then: the epilogue waits for them too, unless it gave up
+      mbar_wait(drain_bar, 0);
     }
     __syncwarp();
   } else if (warp >= 4 && threadIdx.x < Cfg::kFirstLoader) {

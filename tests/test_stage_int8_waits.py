@@ -35,3 +35,10 @@ def test_warps_give_up_as_one():
         assert any("lane == 0" in b for b in blocks), call
     for call, blocks in calls("mbar_wait_warp"):
         assert not any("lane == 0" in b for b in blocks), call
+
+
+def test_copies_and_products_end_before_the_block():
+    """Also those of a role that did not give up itself: nothing conditional on `dead` alone stands around the last waits."""
+    for call, blocks in calls("mbar_wait"):
+        if "drain_bar" in call or "n % S" in call:
+            assert "if (dead)" not in blocks, call
