@@ -156,6 +156,32 @@ ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, c
  */
 int32_t *stage_status_word(void);
 
+/*
+ * What ssn_last_kernel() says after a call of this header: family | (variant << 8).
+ *   STAGE_KERNEL_ROPE       variant: columns per piece (1 .. 8) | the bits below.  The gains' sums are not told apart
+ *   STAGE_KERNEL_DISTILL    CTAs per row (1 .. 8) | STAGE_KVAR_MANY (256 threads) | STAGE_KVAR_GRAD
+ *   STAGE_KERNEL_QUANTIZE   pieces per thread | warps per row << 4; 0: rows of any length and place
+ *   STAGE_KERNEL_INT8_DOT   tokens (1, 2) | STAGE_KVAR_ANYWHERE
+ *   STAGE_KERNEL_INT8_UMMA  rows of the tile's B operand (16 .. 256) | STAGE_KVAR_PAIR, _SWAP, _SPLIT, _ANYWHERE
+ */
+enum {
+  STAGE_KERNEL_ROPE = 16,
+  STAGE_KERNEL_DISTILL = 17,
+  STAGE_KERNEL_QUANTIZE = 18,
+  STAGE_KERNEL_INT8_DOT = 19,
+  STAGE_KERNEL_INT8_UMMA = 20
+};
+#define STAGE_KVAR_ADJACENT 16 /* ROPE: pairs of adjacent columns                                   */
+#define STAGE_KVAR_CROSSED 32  /* ROPE: halves whose partners are read from shared memory           */
+#define STAGE_KVAR_FULL 64     /* ROPE: every column turns                                          */
+#define STAGE_KVAR_BACK 128    /* ROPE: the gradients                                               */
+#define STAGE_KVAR_MANY 16     /* DISTILL                                                           */
+#define STAGE_KVAR_GRAD 32     /* DISTILL                                                           */
+#define STAGE_KVAR_PAIR 1      /* INT8_UMMA: two CTAs per tile                                      */
+#define STAGE_KVAR_SWAP 2      /* INT8_UMMA: the weights on the M side                              */
+#define STAGE_KVAR_SPLIT 4     /* INT8_UMMA: a cluster shares the inner dimension                   */
+#define STAGE_KVAR_ANYWHERE 8  /* INT8: operand rows off 16-byte boundaries                         */
+
 /* ---- the same calls with their arguments in one struct ---------------------------------------------- */
 
 /*

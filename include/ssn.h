@@ -425,6 +425,7 @@ int64_t ssn_launch_count(void);
  * Diagnostic: which kernel the calling thread's most recent codec launch used, as
  * family | (variant bits << 8); SSN_KERNEL_NONE before the first launch.  No counterpart in
  * the paper; the tests use it to assert that a shape reaches the kernel it is meant to check.
+ * The stage operators' kernels have families of their own (STAGE_KERNEL_*, agora_stage.h).
  */
 enum {
   SSN_KERNEL_NONE = 0,

@@ -55,6 +55,10 @@ class ssn_codec_t(ctypes.Structure):
 STAGE_PAIR_HALVES, STAGE_PAIR_ADJACENT = 0, 1
 PAIRINGS = {"halves": STAGE_PAIR_HALVES, "adjacent": STAGE_PAIR_ADJACENT}
 STAGE_MAX_HEAD_DIM, STAGE_DISTILL_MAX_TOP, STAGE_INT8_MAX_INNER = 256, 1024, 131071
+(STAGE_KERNEL_ROPE, STAGE_KERNEL_DISTILL, STAGE_KERNEL_QUANTIZE, STAGE_KERNEL_INT8_DOT, STAGE_KERNEL_INT8_UMMA) = range(16, 21)
+STAGE_KVAR_ADJACENT, STAGE_KVAR_CROSSED, STAGE_KVAR_FULL, STAGE_KVAR_BACK = 16, 32, 64, 128
+STAGE_KVAR_MANY, STAGE_KVAR_GRAD = 16, 32
+STAGE_KVAR_PAIR, STAGE_KVAR_SWAP, STAGE_KVAR_SPLIT, STAGE_KVAR_ANYWHERE = 1, 2, 4, 8
 
 
 class stage_qk_rope_t(ctypes.Structure):

@@ -384,6 +384,7 @@ template <typename T, int kThreads, bool GRAD> cudaError_t launch_threads(const 
   int cluster = 1;   // CTAs per row, while there are SMs without one and pieces enough for it
   while (cluster < kMaxCluster && a.n * cluster <= sms && a.vocab / (Piece<T>::E * cluster * 2) >= 2 * kThreads) cluster *= 2;
   const int64_t workers = a.n < cap / cluster ? a.n : cap / cluster;
+  note_kernel(STAGE_KERNEL_DISTILL, cluster | (kThreads == 256 ? STAGE_KVAR_MANY : 0) | (GRAD ? STAGE_KVAR_GRAD : 0));
   return launch_dependent(distill_kernel<T, kThreads, GRAD>, (unsigned)(workers * cluster), kThreads, 0, stream, cluster, a);
 }
 

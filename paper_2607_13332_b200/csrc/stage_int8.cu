@@ -150,19 +150,24 @@ __global__ void __launch_bounds__(kQuantThreads) int8_quantize_kernel(const Quan
   }
 }
 
+template <typename T, int NV, int WARPS> cudaError_t launch_rows(const QuantArgs &a, cudaStream_t stream) {
+  note_kernel(STAGE_KERNEL_QUANTIZE, NV | WARPS << 4);
+  return launch_dependent(int8_quantize_rows_kernel<T, NV, WARPS>, (unsigned)a.rows, WARPS * 32, 0, stream, 1, a);
+}
+
 template <typename T> cudaError_t launch_quantize(const QuantArgs &a, cudaStream_t stream) {
   constexpr int E = 16 / (int)sizeof(T);
   const bool rows16 = aligned_to(a.x, 16) && (a.rows == 1 || a.ldx % E == 0) && aligned_to(a.q, E) && (a.rows == 1 || a.ldq % E == 0);
   const int64_t pieces = (a.cols + E - 1) / E;
   if (rows16 && pieces <= 4096 && a.rows <= 0x7fffffff) {
-    const unsigned rows = (unsigned)a.rows;
-    if (pieces <= 128) return launch_dependent(int8_quantize_rows_kernel<T, 2, 2>, rows, 64, 0, stream, 1, a);
-    if (pieces <= 256) return launch_dependent(int8_quantize_rows_kernel<T, 4, 2>, rows, 64, 0, stream, 1, a);
-    if (pieces <= 512) return launch_dependent(int8_quantize_rows_kernel<T, 4, 4>, rows, 128, 0, stream, 1, a);
-    if (pieces <= 1024) return launch_dependent(int8_quantize_rows_kernel<T, 4, 8>, rows, 256, 0, stream, 1, a);
-    if (pieces <= 2048) return launch_dependent(int8_quantize_rows_kernel<T, 4, 16>, rows, 512, 0, stream, 1, a);
-    return launch_dependent(int8_quantize_rows_kernel<T, 8, 16>, rows, 512, 0, stream, 1, a);
+    if (pieces <= 128) return launch_rows<T, 2, 2>(a, stream);
+    if (pieces <= 256) return launch_rows<T, 4, 2>(a, stream);
+    if (pieces <= 512) return launch_rows<T, 4, 4>(a, stream);
+    if (pieces <= 1024) return launch_rows<T, 4, 8>(a, stream);
+    if (pieces <= 2048) return launch_rows<T, 4, 16>(a, stream);
+    return launch_rows<T, 8, 16>(a, stream);
   }
+  note_kernel(STAGE_KERNEL_QUANTIZE, 0);
   const int64_t cap = (int64_t)stage_sm_count() * 8;
   return launch_dependent(int8_quantize_kernel<T>, (unsigned)(a.rows < cap ? a.rows : cap), kQuantThreads, 0, stream, 1, a);
 }
@@ -227,6 +232,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) int8_few_kernel(const Int8Matm
 
 template <typename T, bool ANYWHERE> cudaError_t launch_few(const Int8Matmul &a, cudaStream_t stream) {
   const unsigned grid = (unsigned)((a.outer + kFewWarps * kChannels - 1) / (kFewWarps * kChannels));
+  note_kernel(STAGE_KERNEL_INT8_DOT, (int)a.n | (ANYWHERE ? STAGE_KVAR_ANYWHERE : 0));
   if (a.n == 1) return launch_dependent(int8_few_kernel<T, 1, ANYWHERE>, grid, kFewWarps * 32, 0, stream, 1, a);
   return launch_dependent(int8_few_kernel<T, 2, ANYWHERE>, grid, kFewWarps * 32, 0, stream, 1, a);
 }

@@ -33,6 +33,8 @@ cudaError_t launch_tiles(const Int8Matmul &m, int split, int sm_count, cudaStrea
   a.tiles_a = (int32_t)((ra + 128 * CG - 1) / (128 * CG));
   a.tiles_b = (int32_t)((rb + BN - 1) / BN);
   a.dev_status = m.dev_status;
+  note_kernel(STAGE_KERNEL_INT8_UMMA, BN | (CG == 2 ? STAGE_KVAR_PAIR : 0) | (SWAP ? STAGE_KVAR_SWAP : 0) | (split > 1 ? STAGE_KVAR_SPLIT : 0) |
+                                          (RAGGED ? STAGE_KVAR_ANYWHERE : 0));
   cudaError_t e = allow_dynamic_smem(kernel, Cfg::kSmemBytes, allowed);
   if (e != cudaSuccess) return e;
   const int cluster = CG == 2 ? 2 : split;

@@ -557,6 +557,8 @@ cudaError_t launch_unit(const RopeArgs &a, cudaStream_t stream) {
   constexpr int P = BACK ? kBackAhead : kForwardAhead;
   constexpr int kRing = kWarps * P * (BACK ? 2 : 1) * NU * 2 * 32 * V * (int)sizeof(T);
   auto kernel = qk_rope_kernel<T, V, NU, PAIRS, BACK, FULL>;
+  note_kernel(STAGE_KERNEL_ROPE, V | (PAIRS == ADJACENT ? STAGE_KVAR_ADJACENT : PAIRS == CROSSED ? STAGE_KVAR_CROSSED : 0) |
+                                     (FULL ? STAGE_KVAR_FULL : 0) | (BACK ? STAGE_KVAR_BACK : 0));
   const cudaError_t e = allow_dynamic_smem(kernel, kRing + kWarps * (P + 1) * STAGE_MAX_HEAD_DIM * 4, allowed);
   if (e != cudaSuccess) return e;
   return launch_dependent(kernel, (unsigned)(a.side[0].blocks + a.side[1].blocks), kThreads, kRing + kWarps * (P + 1) * a.table_bytes, stream, 1, a);
