@@ -22,10 +22,14 @@ _CODES = {torch.float32: binding.SSN_F32, torch.bfloat16: binding.SSN_BF16}
 
 # Calls of one token are shorter on the GPU than on the host, so every call asks each tensor once for its type, device, shape
 # and strides, and makes its outputs with the cheapest allocation there is: (shape, strides, type) on the current device, 0.9 us
-# against 1.8 to 3.5 us for torch.empty.
-_current_device = torch._C._cuda_getDevice
-_new = torch._C._dynamo.guards._empty_strided_cuda
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# against 1.8 to 3.5 us for torch.empty.  These are private names of torch, which another version may not have.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+try:
+    _new = torch._C._dynamo.guards._empty_strided_cuda
+except AttributeError:
+    def _new(shape, strides, dtype):
+        return torch.empty_strided(shape, strides, dtype=dtype, device="cuda")
 
 
 def _here(t: torch.Tensor, dtype: torch.dtype, what: str) -> torch.Tensor:

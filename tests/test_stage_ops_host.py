@@ -47,3 +47,21 @@ def test_calls_without_a_status_word_share_the_librarys(host, monkeypatch):
         host.distill_loss(logits, ids, top, dev_status=word)
         host.distill_loss_grad(logits, ids, top, dev_status=word)
         assert seen == [want] * 3
+
+
+def test_without_the_private_names_of_torch(host, monkeypatch):
+    """Another version of torch may not have them: the public ones do the same."""
+    import importlib.util
+    for name in ("_cuda_getDevice", "_cuda_getCurrentRawStream"):
+        monkeypatch.delattr(torch._C, name)
+    monkeypatch.delattr(torch._C._dynamo.guards, "_empty_strided_cuda")
+    spec = importlib.util.spec_from_file_location("paper_2607_13332_b200.stage_ops_again", host.__file__)
+    again = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(again)
+    assert again._current_device is torch.cuda.current_device
+    made = []
+    monkeypatch.setattr(torch, "empty_strided", lambda *args, **kw: made.append((args, kw)))
+    again._new((3, 8), (9, 1), torch.int8)
+    assert made == [(((3, 8), (9, 1)), {"dtype": torch.int8, "device": "cuda"})]
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: type("Stream", (), {"cuda_stream": 77 + device}))
+    assert again._raw_stream(1) == 78
