@@ -162,7 +162,7 @@ struct __align__(16) Part {   // one CTA's share of a row
 struct Shared {
   MaxSum ms[kMaxWarps];
   Teacher teacher[kMaxWarps];
-  Part ctas[2][kMaxCluster];            // rows take turns
+  Part ctas[kMaxCluster];               // written once: a cluster has one row
   int32_t id[STAGE_DISTILL_MAX_TOP];    // -1: padding, or another CTA's column
   float e[STAGE_DISTILL_MAX_TOP];       // relative to the maximum of the warp that has the entry
   float at[STAGE_DISTILL_MAX_TOP];      // the student's logit there
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
   if (cluster > 1) cluster_sync();   // the peers have started: their shared memory may be written
   pdl_enter();
   const int64_t workers = gridDim.x / cluster;
-  int turn = 0, next_id = -1;
+  int next_id = -1;
   float next_top = 0.f, next_w = 1.f;
   auto look = [&](int64_t t) {
     if (t >= a.n) return;
@@ -314,17 +314,16 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
     if (cluster > 1) {
       if (warp == 0) {
         if (lane < (int)cluster) {   // to the CTA of that rank
-          const uint32_t to = map_to_rank(smem_address(&sh.ctas[turn][rank]), (uint32_t)lane);
+          const uint32_t to = map_to_rank(smem_address(&sh.ctas[rank]), (uint32_t)lane);
           asm volatile("st.shared::cluster.f64 [%0], %1;\n" ::"r"(to), "d"(ta) : "memory");
           asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};\n" ::"r"(to + 8), "f"(ms.m), "f"(ms.l) : "memory");
         }
         __syncwarp();
       }
       cluster_sync();
-      ms = merge_warp(lane < (int)cluster ? sh.ctas[turn][lane].ms : MaxSum{-INFINITY, 0.f}, scale);
+      ms = merge_warp(lane < (int)cluster ? sh.ctas[lane].ms : MaxSum{-INFINITY, 0.f}, scale);
       ta = 0.0;
-      for (int i = 0; i < (int)cluster; ++i) ta += sh.ctas[turn][i].a;
-      turn ^= 1;
+      for (int i = 0; i < (int)cluster; ++i) ta += sh.ctas[i].a;
     }
     if (tid == 0 && rank == 0) {
       // log p = (top - top_m) / tau - log tsum, the student's log sum is m / tau + log l
@@ -381,7 +380,10 @@ __global__ void __launch_bounds__(kThreads, per_sm(kThreads, GRAD)) distill_kern
 template <typename T, int kThreads, bool GRAD> cudaError_t launch_threads(const DistillArgs &a, cudaStream_t stream) {
   const int sms = stage_sm_count();
   const int64_t cap = (int64_t)sms * per_sm(kThreads, GRAD);
-  int cluster = 1;   // CTAs per row, while there are SMs without one and pieces enough for it
+  // CTAs per row: doubled while there are no more of them than SMs, and while each keeps pieces enough.  That leaves two CTAs per SM at
+  // most, which are all resident, so that a cluster takes one row and no more.
+  static_assert(per_sm(kThreads, GRAD) >= 2, "a cluster would take a second row");
+  int cluster = 1;
   while (cluster < kMaxCluster && a.n * cluster <= sms && a.vocab / (Piece<T>::E * cluster * 2) >= 2 * kThreads) cluster *= 2;
   const int64_t workers = a.n < cap / cluster ? a.n : cap / cluster;
   note_kernel(STAGE_KERNEL_DISTILL, cluster | (kThreads == 256 ? STAGE_KVAR_MANY : 0) | (GRAD ? STAGE_KVAR_GRAD : 0));
