@@ -168,24 +168,4 @@ template <int V> __device__ __forceinline__ float v_total(const float (&a)[V]) {
   }
 }
 
-// V floats of a 16-byte aligned (V >= 4) or V * 4-byte aligned table row
-template <int V> __device__ __forceinline__ void load_floats(const float *p, float (&x)[V]) {
-  if constexpr (V >= 4) {
-#pragma unroll
-    for (int i = 0; i < V; i += 4) {
-      const float4 f = __ldg(reinterpret_cast<const float4 *>(p + i));
-      x[i] = f.x;
-      x[i + 1] = f.y;
-      x[i + 2] = f.z;
-      x[i + 3] = f.w;
-    }
-  } else if constexpr (V == 2) {
-    const float2 f = __ldg(reinterpret_cast<const float2 *>(p));
-    x[0] = f.x;
-    x[1] = f.y;
-  } else {
-    x[0] = __ldg(p);
-  }
-}
-
 }  // namespace ssn
