@@ -264,8 +264,14 @@ def distill_loss_grad(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor
     logits; made here, its rows stand as close together as keeps them as far from 16-byte boundaries as the logits' rows."""
     if dlogits is None:
         n, vocab = logits.shape
+        size = logits.element_size()
         ld = _pitch(_here(logits, logits.dtype, "logits"), n, vocab)      # of a view, any number of rows
-        dlogits = _new((n, vocab), (vocab + (ld - vocab) % (16 // logits.element_size()), 1), logits.dtype)
+        ld = vocab + (ld - vocab) % (16 // size)
+        at = logits.data_ptr() % 16 // size
+        if at == 0:
+            dlogits = _new((n, vocab), (ld, 1), logits.dtype)
+        else:
+            dlogits = _new((at + max(n - 1, 0) * ld + vocab,), (1,), logits.dtype).as_strided((n, vocab), (ld, 1), at)
     return _distill(logits, ids, top, weight, temperature, dlogits, dev_status), dlogits
 
 

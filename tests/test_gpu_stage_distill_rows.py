@@ -53,3 +53,16 @@ def test_last_tokens_of_sequences(vocab):
     loss, grad = distill_loss_grad(last, ids[:24], top[:24], weight[:24])
     assert_rows(last, ids[:24], top[:24], weight[:24], 1.0, loss, grad)
     assert grad.untyped_storage().nbytes() <= 24 * (vocab + 8) * 2
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_logits_that_start_off_a_boundary(dtype):
+    """Logits without their first rows, an odd vocabulary: the gradient made by the call is the one of a caller's buffer."""
+    rng = np.random.default_rng(31)
+    logits, ids, top, weight = make(rng, 12, 2003, 16, dtype)
+    for first in range(8):
+        args = logits[first:], ids[first:], top[first:], weight[first:]
+        loss, grad = distill_loss_grad(*args)
+        assert_rows(*args, 1.0, loss, grad)
+        loss2, grad2 = distill_loss_grad(*args, dlogits=torch.empty_like(args[0]))
+        assert torch.equal(loss, loss2) and torch.equal(grad, grad2)

@@ -14,6 +14,18 @@ def host(libssn, monkeypatch):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_gradient_lies_as_its_logits_do(host, monkeypatch, dtype):
+    """Wherever the logits start, so that the kernel stores whole pieces."""
+    monkeypatch.setattr(host, "_distill", lambda *args: None)
+    buf = torch.zeros(4000, dtype=dtype)
+    for logits in [buf[1:].view(31, 129)[i:] for i in range(9)] + [buf[i:i + 800].view(8, 100)[:, j:j + 90] for i in range(8) for j in (0, 3)] + [buf[5:105].view(1, 100)]:
+        dlogits = host.distill_loss_grad(logits, None, None)[1]
+        assert dlogits.shape == logits.shape and dlogits.stride(1) == 1
+        assert all((dlogits[t].data_ptr() - logits[t].data_ptr()) % 16 == 0 for t in range(len(logits)))
+        assert dlogits.untyped_storage().nbytes() <= len(logits) * (logits.shape[1] * dtype.itemsize + 16) + 16
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("vocab", [1, 7, 96, 101])
 def test_a_gradient_takes_no_more_room_than_its_rows(host, monkeypatch, dtype, vocab):
     monkeypatch.setattr(host, "_distill", lambda *args: None)
