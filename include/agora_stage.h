@@ -61,7 +61,8 @@ ssn_status_t stage_rope_table(float *table, int64_t ldt, int32_t max_pos, int32_
  *     n = x / sqrt(mean(x^2) + eps) * w;     y = n with its column pairs (a, b) turned by the angle of pos(t):
  *     (a cos - b sin, b cos + a sin)
  *   q, k     [n_tokens x heads x D], D contiguous; any strides >= 0 (views of a fused projection's output,
- *            head-major buffers, broadcast rows).  0 heads: that tensor is absent and may be NULL.
+ *            head-major buffers, broadcast rows), at most 65536 heads.  0 heads: that tensor is absent and may be NULL.
+ *            The squares are summed in fp32: a row whose sum passes its range (values around 10^18) becomes zeros.
  *   q_out, k_out   the same with strides that keep its rows apart.  An output may be its own input
  *            (same address and strides).
  *   pos      device int32[n_tokens], or NULL: pos(t) = t mod seq_len (seq_len >= 1 required then).
@@ -114,6 +115,9 @@ ssn_status_t stage_qk_rope_backward(const stage_qk_rope_t *op, const void *dq, i
  *            (same address and ldd == ldl).
  * A row of weight 0, one without entries and one whose entries are all -inf have loss 0 and a gradient of zeros,
  * whatever their logits hold.  Logits of -inf have probability 0 (a loss of +inf where the teacher gives them any).
+ * With top_k = 1 and tau = 1 it is the cross entropy of the target ids[t, 0], whatever finite number its teacher logit is.
+ * The loss has the same bits with the gradient and without.  The order of a row's sums goes by the number of rows (few rows are
+ * shared by several CTAs) and by the row's place within 16 bytes.
  */
 ssn_status_t stage_distill_loss(const void *logits, int64_t ldl, int32_t dtype, int64_t n_tokens, int64_t vocab,
                                 const int32_t *ids, int64_t ldi, const float *top, int64_t ldt, int32_t top_k,
@@ -142,7 +146,7 @@ ssn_status_t stage_int8_quantize(const void *x, int64_t ldx, int32_t dtype, int6
  *   ws  fp32 [outer];  y  [n_tokens x outer] of dtype, ldy >= outer;  1 <= inner <= STAGE_INT8_MAX_INNER
  *   dev_status  device int32 or NULL: SSN_DEV_TIMEOUT when an internal bounded wait ran out (y is invalid then)
  * Any int8 value may occur, -128 too.  Rows that start on 16-byte boundaries (address and leading dimension of xq and wq) are
- * fetched by TMA; with others the product takes about five times as long.  Any y will do; rows on 16-byte boundaries are
+ * fetched by TMA; with others the product takes twice as long (few tokens) to eight times (many).  Any y will do; rows on 16-byte boundaries are
  * stored 16 bytes at a time.
  */
 ssn_status_t stage_int8_matmul(const int8_t *xq, int64_t ldx, const float *xs, const int8_t *wq, int64_t ldw,

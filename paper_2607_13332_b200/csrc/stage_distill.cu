@@ -4,9 +4,10 @@
 // the gradient is w tau exp((s - m) / tau) / L, minus w tau p at the teacher's ids.  The loss reads the row once; the
 // gradient reads it once more out of L2 and writes it once, so that HBM sees the row read once and written once.
 //
-// What bounds it: HBM for the loss of long rows (2048 x 128256 bf16 in 100 us, 5.2 TB/s).  The gradient (8192 x 128256 bf16 in
-// 0.95 ms, 4.4 TB/s) also waits for its exponentials, two per element on a pipe of 16 lanes per clock and SM, and for the
-// reductions between the passes.  Tried and dropped: the exponentials of a row kept in the registers of a cluster of eight
+// What bounds it: HBM for the loss of long rows (2048 x 128256 bf16 in 100 us, 5.2 TB/s; fp32 in 186, 5.6).  The gradient (8192 x
+// 128256 bf16 in 0.97 ms, 4.3 TB/s) fills neither HBM (56 % in a capture) nor the pipe of its exponentials (54 %; two per element,
+// 16 lanes per clock and SM): a row is two passes with reductions between them, which the few warps that its pieces in flight leave
+// room for (a third of an SM's) do not hide, and part of the second pass misses L2.  Tried and dropped: the exponentials of a row kept in the registers of a cluster of eight
 // CTAs, so that each is computed once (1.44 ms: 33 of the 37 clusters fit, and 20 warps share too little of a row); a ring of
 // bulk copies with a warp of its own (1.01 ms); registers filled a round ahead (fewer warps, slower); bf16 widened by shifts
 // before the subtraction (1.01 against 0.96 ms with four pieces in flight); a quarter of the exponentials by a polynomial on the

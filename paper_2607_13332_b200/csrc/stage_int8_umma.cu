@@ -65,9 +65,10 @@ template <typename T> cudaError_t launch_typed(const Int8Matmul &m, int sms, cud
   if (m.n <= 32) return launch_tiles<1, 32, true, T>(m, split_of(m, 32, sms), sms, stream);
   if (m.n <= 64) return launch_tiles<1, 64, true, T>(m, split_of(m, 64, sms), sms, stream);
   // The shape whose waves of tiles take the least time: a step of a wave of pairs of 256 x 256 takes about 0.38 us, of CTAs of
-  // 128 x 256 0.42 (each loads B for itself), of the narrower ones 0.26; a wave's first loads and a tile's output cost as much as
-  // some 8 and 5 steps.  Measured (us; pairs 256, pairs 128, CTAs 256, CTAs 128): 777 x 2000 x 5003 21.8 / 21.7 / 16.4 / 19.1,
-  // 128 x 4096 x 4096 15.2 / 13.9 / 14.5 / 13.2, 256 x 4096 x 128256 109 / 140 / 128 / 150, 16384 x 256 x 4096 59 / 75 / 52 / 60.
+  // 128 x 256 0.42 (each loads B for itself), of CTAs of 128 x 128 0.28; the output of a tile takes 4.0, 3.5 and 3.0 us, which
+  // is also the least time of a wave, and is hidden behind the next wave but for the last one.  Measured (us; pairs, CTAs of 256,
+  // CTAs of 128): 777 x 2000 x 5003 21.8 / 16.4 / 19.1, 128 x 4096 x 4096 15.2 / 14.5 / 13.2, 256 x 4096 x 128256 109 / 128 / 150,
+  // 16384 x 256 x 4096 59 / 52 / 60.
   const double steps = (double)((m.inner + kInt8Step - 1) / kInt8Step);
   auto time = [&](int64_t ta, int64_t bn, int64_t workers, double step, double rest) {
     const int64_t tiles = ta * ((m.outer + bn - 1) / bn), waves = (tiles + workers - 1) / workers;

@@ -1,5 +1,8 @@
 """Torch-tensor sugar over the model operators of a stage (include/agora_stage.h): argument marshalling only, every step
-runs in the library's kernels, on the current stream of the current device."""
+runs in the library's kernels, on the current stream of the current device.
+
+Autograd records none of these calls: outputs never require a gradient, whether inputs do or not.  A training step calls forward
+and backward itself, or from a torch.autograd.Function of its own."""
 
 from __future__ import annotations
 
@@ -253,7 +256,8 @@ def _distill(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight:
 def distill_loss(logits: torch.Tensor, ids: torch.Tensor, top: torch.Tensor, weight: Optional[torch.Tensor] = None,
                  temperature: float = 1.0, dev_status: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Loss [n] fp32 of logits [n, vocab] against the teacher's top logits top [n, k] fp32 at ids [n, k] int32 (-1: padding):
-    weight times temperature^2 times the divergence of the student's softmax from the teacher's over its entries.  Ids outside
+    weight times temperature^2 times the divergence of the student's softmax from the teacher's over its entries (with k = 1 and
+    temperature 1 the cross entropy of the targets ids).  Ids outside
     the vocabulary set SSN_DEV_BAD_ID in dev_status (int32 [1]), or in the word that take_status() reads."""
     return _distill(logits, ids, top, weight, temperature, None, dev_status)
 
