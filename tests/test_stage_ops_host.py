@@ -77,3 +77,9 @@ def test_without_the_private_names_of_torch(host, monkeypatch):
     assert made == [(((3, 8), (9, 1)), {"dtype": torch.int8, "device": "cuda"})]
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device: type("Stream", (), {"cuda_stream": 77 + device}))
     assert again._raw_stream(1) == 78
+
+
+def test_without_a_gpu_there_is_no_status_word(libssn):
+    if torch.cuda.is_available():
+        pytest.skip("there is one here")
+    assert libssn.library().stage_status_word() is None
